@@ -527,6 +527,104 @@ int32_t moe_expert_pool_stats(const moe_expert_pool* p, uint64_t* bytes_copied, 
                               uint64_t* hits, uint64_t* misses, uint64_t* evictions);
 int32_t moe_expert_pool_destroy(moe_expert_pool* p);
 
+/* ---- the attention half of a decoded token -------------------------------- */
+/*
+ * What a generated token passes before the MoE layer of its block: rotary positions of its query and key, the
+ * append of its key and value to a paged cache, and its attention over that cache.  Same rules as above: caller-owned
+ * device memory, no allocation, no synchronisation, arguments validated before any launch, one HIP stream.
+ */
+
+/* Rows of a [tokens, heads, head_dim] tensor with strides in elements (a token's queries inside the output of a
+ * fused projection, say); a head's head_dim elements are contiguous. */
+typedef struct {
+  void* data;
+  int64_t token_stride;
+  int64_t head_stride;
+} moe_head_rows;
+
+#define MOE_MAX_ROTARY_AXES 3
+#define MOE_MAX_HEAD_DIM 256
+#define MOE_MAX_HEADS (1 << 17)
+
+/* Rotary positions of a head: the first rot_dim of its head_dim elements are rot_dim/2 pairs, pair i being elements
+ * (i, i + rot_dim/2), or (2i, 2i+1) if interleaved; the others pass through.  Pair i turns by the angle
+ * position[axis of i] * freqs[i] radians.  The pairs belong to the axes in order: axis_pairs[0] pairs to the first
+ * (time), then axis_pairs[1] (height), axis_pairs[2] (width); text has n_axes = 1. */
+typedef struct {
+  int32_t head_dim;    /* 2..MOE_MAX_HEAD_DIM                                       */
+  int32_t rot_dim;     /* even, 2..head_dim                                         */
+  int32_t interleaved; /* 0 or 1                                                    */
+  int32_t n_axes;      /* 1..MOE_MAX_ROTARY_AXES                                    */
+  int32_t axis_pairs[MOE_MAX_ROTARY_AXES]; /* sum over the n_axes = rot_dim/2       */
+  const double* freqs; /* device float64 [rot_dim/2]                                */
+} moe_rotary_spec;
+
+/* out[t,h] = x[t,h] with its pairs rotated: (a, b) -> (a cos - b sin, a sin + b cos).  inverse = 1 turns the other
+ * way, which is the gradient as well: with d_out for x it gives d_x.  The angle is taken in float64 and reduced to
+ * one turn (positions of any size keep their angle), cosine, sine and rotation are float32, rounded once to dtype.
+ * x, out [T, n_heads, head_dim] of dtype (moe_dtype); out may be x itself (same data and strides), and must not
+ * overlap it otherwise.  positions device int32 [n_axes, T], any sign. */
+int32_t moe_rotary(const moe_rotary_spec* r, int32_t dtype, int32_t T, int32_t n_heads, const moe_head_rows* x,
+                   const int32_t* positions, const moe_head_rows* out, int32_t inverse, void* stream);
+
+/* A paged cache of keys and values of n_seqs sequences: place p of sequence s is row p % page_size of page
+ * page_table[s, p / page_size].  The key of kv head h there starts at
+ *   k + page*page_stride + (p % page_size)*token_stride + h*head_stride     (elements; v with the same strides)
+ * so pages may be [page_size, heads, head_dim] or [heads, page_size, head_dim], and keys and values may share a pool.
+ * A table entry outside 0..n_pages-1 is a page that is not there: nothing is written to it, and attention leaves its
+ * keys out.  The device pointers and the strides are multiples of 16 bytes, and so is a head's row. */
+typedef struct {
+  void* k;
+  void* v;
+  const int32_t* page_table; /* device int32 [n_seqs, table_width]                                    */
+  int64_t n_pages;           /* 0..INT32_MAX                                                          */
+  int64_t page_stride, token_stride, head_stride;
+  int32_t page_size;         /* >= 1; table_width*page_size <= INT32_MAX                              */
+  int32_t n_seqs, table_width;
+  int32_t n_kv_heads;        /* 1..MOE_MAX_HEADS                                                      */
+  int32_t head_dim;          /* multiple of 8 (MOE_BF16) or 4 (MOE_F32), at most MOE_MAX_HEAD_DIM     */
+  int32_t dtype;             /* moe_dtype of keys, values, queries and outputs                        */
+} moe_kv_cache;
+
+/* Validates a cache (same checks as the calls that take one). */
+int32_t moe_kv_cache_check(const moe_kv_cache* c);
+
+/* Keys and values of T new tokens into their places: token t is place cache_pos[t] of sequence token_seq[t]
+ * (token_seq NULL: of sequence t, T <= n_seqs).  A place or sequence outside the table, or on a page that is not
+ * there, writes nothing.  No two tokens of a call may have one place.
+ * r (nullable): keys are rotated on the way, and the queries q [T, n_q_heads, head_dim] (nullable) of the same tokens
+ * into q_out (may be q itself), for every token, whether its place is there or not.  positions device int32
+ * [n_axes, T]; NULL: cache_pos (n_axes = 1).  r NULL: keys are stored as they are, and q must be NULL.
+ * k, v [T, n_kv_heads, head_dim]; cache_pos, token_seq device int32 [T]. */
+int32_t moe_kv_append(const moe_kv_cache* c, int32_t T, const moe_head_rows* k, const moe_head_rows* v,
+                      const int32_t* token_seq, const int32_t* cache_pos, const moe_rotary_spec* r,
+                      const int32_t* positions, int32_t n_q_heads, const moe_head_rows* q, const moe_head_rows* q_out,
+                      void* stream);
+
+typedef struct {
+  float scale;         /* of the scores, usually head_dim^-1/2                                    */
+  float softcap;       /* > 0: scores are capped, softcap*tanh(score/softcap); 0: not             */
+  int32_t window;      /* > 0: only the last `window` places of a sequence are attended; 0: all   */
+  const float* slopes; /* nullable: device float [n_q_heads], score -= slope*(distance to the new token) */
+} moe_attention_options;
+
+/* Attention of one new token per sequence.  Sequence s has seq_lens[s] places in the cache (device int32 [n_seqs];
+ * clamped to 0..table_width*page_size), the last of them being the new token's own.  For query head h, with keys and
+ * values of kv head h / (n_q_heads/n_kv_heads), over the kept places j (inside the window, on a page that is there):
+ *   z_j = scale*<q_h, k_j>, capped, minus slope_h*(seq_lens[s]-1-j)
+ *   lse = log sum_j exp(z_j)        out_h = sum_j exp(z_j - lse) v_j
+ * No place kept, or no score above -infinity: out_h = 0, lse = -infinity.  What lies in places that are not kept (NaN
+ * and infinities among it) reaches no output.  Products of MOE_BF16 are exact and accumulated in float32, softmax
+ * weights enter with 16 bits of mantissa, out is rounded once.
+ * q, out [n_seqs, n_q_heads, head_dim], pointers and strides multiples of 16 bytes; n_q_heads a multiple of
+ * n_kv_heads; lse (nullable) device float [n_seqs, n_q_heads].  ws: moe_attention_decode_workspace_bytes, 256-byte
+ * aligned, need not be cleared, one call at a time.  Results do not depend on what else runs: the split over the
+ * length follows from the lengths alone, and its parts are joined in order. */
+size_t moe_attention_decode_workspace_bytes(const moe_kv_cache* c, int32_t n_q_heads);
+int32_t moe_attention_decode(const moe_kv_cache* c, int32_t n_q_heads, const moe_head_rows* q, const int32_t* seq_lens,
+                             const moe_attention_options* opt, const moe_head_rows* out, float* lse, void* ws,
+                             size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -9,3 +9,6 @@ from .binding import (  # noqa: F401
     moe_layer_forward_timed, moe_layer_route, moe_layer_experts, moe_transpose_expert_weights, moe_workspace_bytes, moe_workspace_layout,
     STAGE_NAMES, MOE_TUNE_GEMM_TILE_ROWS, MOE_TUNE_FEW_TOKEN_KERNELS, MOE_TUNE_GATE_TOKENS, MOE_TUNE_GEMM_MFMA, moe_get_tuning, moe_set_tuning,
 )
+from .attention import (  # noqa: F401
+    KVCache, Rotary, moe_attention_decode, moe_attention_decode_workspace_bytes, moe_kv_append, moe_rotary, rotary_freqs,
+)

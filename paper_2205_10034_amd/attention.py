@@ -1,0 +1,201 @@
+"""ctypes binding of the attention half of a decoded token: rotary positions, the append to a paged cache and the
+attention that reads it.  Argument marshalling only, as in :mod:`.binding`; functions have the names and meanings of
+their C counterparts in ``include/moesys.h``.
+
+Tensors of tokens are ``[tokens, heads, head_dim]`` CUDA tensors whose last dimension is contiguous; the other two may
+have any strides (the queries inside the output of a fused projection).
+"""
+from __future__ import annotations
+
+import ctypes as C
+from typing import Optional, Sequence
+
+import torch
+
+from . import binding as B
+
+_MAX_AXES = 3
+
+
+class _HeadRows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class _RotarySpec(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("n_axes", C.c_int32),
+                ("axis_pairs", C.c_int32 * _MAX_AXES), ("freqs", C.c_void_p)]
+
+
+class _Cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_table", C.c_void_p), ("n_pages", C.c_int64),
+                ("page_stride", C.c_int64), ("token_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("page_size", C.c_int32), ("n_seqs", C.c_int32), ("table_width", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32)]
+
+
+class _Options(C.Structure):
+    _fields_ = [("scale", C.c_float), ("softcap", C.c_float), ("window", C.c_int32), ("slopes", C.c_void_p)]
+
+
+_DTYPES = {torch.float32: B.MOE_F32, torch.bfloat16: B.MOE_BF16}
+_lib = None
+
+
+def lib() -> C.CDLL:
+    """The library with this module's argument types set."""
+    global _lib
+    if _lib is None:
+        L = B.lib()
+        vp, rows = C.c_void_p, C.POINTER(_HeadRows)
+        L.moe_kv_cache_check.argtypes = [C.POINTER(_Cache)]
+        L.moe_rotary.argtypes = [C.POINTER(_RotarySpec), C.c_int32, C.c_int32, C.c_int32, rows, vp, rows, C.c_int32, vp]
+        L.moe_kv_append.argtypes = [C.POINTER(_Cache), C.c_int32, rows, rows, vp, vp, C.POINTER(_RotarySpec), vp, C.c_int32, rows, rows, vp]
+        L.moe_attention_decode_workspace_bytes.restype = C.c_size_t
+        L.moe_attention_decode_workspace_bytes.argtypes = [C.POINTER(_Cache), C.c_int32]
+        L.moe_attention_decode.argtypes = [C.POINTER(_Cache), C.c_int32, rows, vp, C.POINTER(_Options), rows, vp, vp, C.c_size_t, vp]
+        _lib = L
+    return _lib
+
+
+def _dtype(t) -> int:
+    if t.dtype not in _DTYPES:
+        raise ValueError(f"{t.dtype} tensors: float32 and bfloat16 are supported")
+    return _DTYPES[t.dtype]
+
+
+def _rows(t, what: str, shape, dtype) -> _HeadRows:
+    """[tokens, heads, head_dim] as the library takes it, checked against what the call says it holds."""
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{what} has shape {tuple(t.shape)}, the call needs {shape}")
+    if t.dtype != dtype:
+        raise ValueError(f"{what} is {t.dtype}, the call needs {dtype}")
+    st, sh, sd = t.stride()
+    if sd != 1 and shape[2] > 1:
+        raise ValueError(f"{what}: the elements of a head must be contiguous")
+    return _HeadRows(t.data_ptr(), st, sh)
+
+
+def _ints(t, what: str, *shapes) -> Optional[int]:
+    """A contiguous int32 tensor of one of the given shapes."""
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or tuple(t.shape) not in shapes or not t.is_contiguous():
+        raise ValueError(f"{what} is a {t.dtype} tensor of shape {tuple(t.shape)}, the call needs a contiguous int32 one of {' or '.join(map(str, shapes))}")
+    return t.data_ptr()
+
+
+def _on_device(*tensors) -> None:
+    first = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("device tensors are needed")
+        first = t.device if first is None else first
+        if t.device != first:
+            raise ValueError(f"tensors on {first} and {t.device}")
+
+
+class Rotary:
+    """Rotary positions of a head (moe_rotary_spec): ``freqs`` is a float64 CUDA tensor of rot_dim/2 radians per position,
+    ``axis_pairs`` how many of the pairs belong to each axis, in order (default: all to one)."""
+
+    def __init__(self, head_dim: int, freqs, axis_pairs: Optional[Sequence[int]] = None, interleaved: bool = False):
+        if freqs.dtype != torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous():
+            raise ValueError("freqs must be a contiguous float64 vector")
+        _on_device(freqs)
+        pairs = [freqs.numel()] if axis_pairs is None else [int(n) for n in axis_pairs]
+        if not 1 <= len(pairs) <= _MAX_AXES:
+            raise ValueError(f"{len(pairs)} axes: 1 to {_MAX_AXES} are supported")
+        self.freqs, self.head_dim, self.n_axes = freqs, head_dim, len(pairs)
+        self.c = _RotarySpec(head_dim, 2 * freqs.numel(), int(bool(interleaved)), len(pairs),
+                             (C.c_int32 * _MAX_AXES)(*(pairs + [0] * (_MAX_AXES - len(pairs)))), freqs.data_ptr())
+
+
+def rotary_freqs(rot_dim: int, base: float = 10000.0, device="cuda"):
+    """The usual geometric series base^(-2i/rot_dim), i < rot_dim/2, in float64."""
+    i = torch.arange(rot_dim // 2, dtype=torch.float64)
+    return (base ** (-2.0 * i / rot_dim)).to(device)
+
+
+class KVCache:
+    """A paged cache of keys and values (moe_kv_cache): ``k`` and ``v`` are pools of pages, [pages, page_size, heads, head_dim]
+    (``token_major``) or [pages, heads, page_size, head_dim] (``head_major``), of one dtype and the same strides (they may be
+    halves of one tensor); ``page_table`` is int32 [sequences, width].  Keeps the tensors, and reads their contents anew in
+    every call."""
+
+    def __init__(self, k, v, page_table, layout: str = "token_major"):
+        if layout not in ("token_major", "head_major"):
+            raise ValueError(f"layout {layout!r}: token_major or head_major")
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.stride() != v.stride():
+            raise ValueError("k and v must be 4-dimensional pools of one shape, dtype and strides")
+        if k.stride(3) != 1:
+            raise ValueError("the elements of a head must be contiguous")
+        if page_table.dtype != torch.int32 or page_table.dim() != 2 or not page_table.is_contiguous():
+            raise ValueError("page_table must be a contiguous int32 matrix")
+        _on_device(k, v, page_table)
+        self.k, self.v, self.page_table, self.layout = k, v, page_table, layout
+        tok, head = (1, 2) if layout == "token_major" else (2, 1)
+        self.page_size, self.n_kv_heads, self.head_dim = k.shape[tok], k.shape[head], k.shape[3]
+        self.n_seqs, self.dtype = page_table.shape[0], k.dtype
+        self.c = _Cache(k.data_ptr() or None, v.data_ptr() or None, page_table.data_ptr() or None, k.shape[0], k.stride(0), k.stride(tok),
+                        k.stride(head), self.page_size, page_table.shape[0], page_table.shape[1], self.n_kv_heads, self.head_dim, _dtype(k))
+        B._check(lib().moe_kv_cache_check(C.byref(self.c)), "moe_kv_cache_check")
+
+
+def moe_rotary(rotary: Rotary, x, positions, out, inverse: bool = False, stream=None):
+    """out <- x [T, heads, head_dim] rotated by positions [axes, T] (int32); ``inverse``: back, or the gradient."""
+    T, H, D = x.shape
+    _on_device(x, positions, out, rotary.freqs)
+    if D != rotary.head_dim:
+        raise ValueError(f"x has heads of {D}, the rotary positions are for {rotary.head_dim}")
+    xr, outr = _rows(x, "x", (T, H, D), x.dtype), _rows(out, "out", (T, H, D), x.dtype)
+    pos = _ints(positions, "positions", (rotary.n_axes, T), *([(T,)] if rotary.n_axes == 1 else []))
+    B._check(lib().moe_rotary(C.byref(rotary.c), _dtype(x), T, H, C.byref(xr), pos, C.byref(outr), int(bool(inverse)), B._stream(stream)), "moe_rotary")
+
+
+def moe_kv_append(cache: KVCache, k, v, cache_pos, token_seq=None, rotary: Optional[Rotary] = None, positions=None, q=None, q_out=None,
+                  stream=None):
+    """Keys and values [T, kv_heads, head_dim] of new tokens into their places of the cache, keys rotated; queries
+    [T, heads, head_dim] rotated into q_out."""
+    T = k.shape[0]
+    _on_device(k, v, cache_pos, token_seq, positions, q, q_out, cache.k, rotary.freqs if rotary is not None else None)
+    kv = (T, cache.n_kv_heads, cache.head_dim)
+    kr, vr = _rows(k, "k", kv, cache.dtype), _rows(v, "v", kv, cache.dtype)
+    qr = qo = None
+    hq = 0
+    if q is not None:
+        if q_out is None:
+            raise ValueError("q without q_out")
+        hq = q.shape[1]
+        qr, qo = _rows(q, "q", (T, hq, cache.head_dim), cache.dtype), _rows(q_out, "q_out", (T, hq, cache.head_dim), cache.dtype)
+    axes = rotary.n_axes if rotary is not None else 1
+    B._check(lib().moe_kv_append(
+        C.byref(cache.c), T, C.byref(kr), C.byref(vr), _ints(token_seq, "token_seq", (T,)), _ints(cache_pos, "cache_pos", (T,)),
+        C.byref(rotary.c) if rotary is not None else None, _ints(positions, "positions", (axes, T), *([(T,)] if axes == 1 else [])), hq,
+        C.byref(qr) if qr is not None else None, C.byref(qo) if qo is not None else None, B._stream(stream)), "moe_kv_append")
+
+
+def moe_attention_decode_workspace_bytes(cache: KVCache, n_q_heads: int) -> int:
+    n = lib().moe_attention_decode_workspace_bytes(C.byref(cache.c), n_q_heads)
+    if n == 0:
+        raise B.MoEError(1, "moe_attention_decode_workspace_bytes", lib().moe_last_error().decode())
+    return n
+
+
+def moe_attention_decode(cache: KVCache, q, seq_lens, out, ws, scale: Optional[float] = None, softcap: float = 0.0, window: int = 0,
+                         slopes=None, lse=None, stream=None):
+    """Attention of one new token per sequence: q, out [sequences, heads, head_dim], seq_lens int32 [sequences] (the new token
+    counted), slopes float32 [heads] (optional), lse float32 [sequences, heads] (optional output)."""
+    S, H, D = cache.n_seqs, q.shape[1], cache.head_dim
+    _on_device(q, seq_lens, out, ws, slopes, lse, cache.k)
+    qr, outr = _rows(q, "q", (S, H, D), cache.dtype), _rows(out, "out", (S, H, D), cache.dtype)
+    for t, what, shape in ((slopes, "slopes", (H,)), (lse, "lse", (S, H))):
+        if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous()):
+            raise ValueError(f"{what} must be a contiguous float32 tensor of shape {shape}")
+    if not ws.is_contiguous():
+        raise ValueError("the workspace must be contiguous")
+    opt = _Options(D ** -0.5 if scale is None else scale, softcap, window, slopes.data_ptr() if slopes is not None else None)
+    B._check(lib().moe_attention_decode(
+        C.byref(cache.c), H, C.byref(qr), _ints(seq_lens, "seq_lens", (S,)), C.byref(opt), C.byref(outr), lse.data_ptr() if lse is not None else None,
+        ws.data_ptr(), ws.numel() * ws.element_size(), B._stream(stream)), "moe_attention_decode")
