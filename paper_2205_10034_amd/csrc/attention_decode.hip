@@ -1,58 +1,467 @@
 // Attention of one new token per sequence over a paged cache (moe_attention_decode): one pass over the keys and values
 // with the running maximum m and sum l of the softmax,
-//   m' = max(m, z_j);  l' = l exp(m - m') + exp(z_j - m');  o' = o exp(m - m') + exp(z_j - m') v_j;  out = o / l.
-// One wavefront per query head.
+//   m' = max(m, z_j);  l' = l exp(m - m') + exp(z_j - m');  o' = o exp(m - m') + exp(z_j - m') v_j;  out = o / l,
+// split over the length into chunks whose (m, l, o) are joined at the end with the weights exp(m_i - max m).
+//
+// Bound: HBM, every key and value once; the arithmetic is G = query heads per kv head multiply-adds per element.  So
+// the kernel is built around loads that go from memory into the registers that the matrix instructions read:
+//  - A wavefront takes tiles of 32 (bfloat16) or 16 (float32) places and the up to 16 query heads of one kv head.
+//  - Scores: S^T[place, head] = K Q^T, keys as the first operand: a lane loads 16 bytes of one key.  The contraction index
+//    of an instruction may be any permutation of the dimensions as long as both operands use it.
+//  - Output: O^T[dim, head] += V^T P^T.  A lane of S^T holds four places of one head, which is how the second operand wants
+//    P^T when the places of an instruction are taken in that order: no data moves between lanes.  The first operand has to
+//    hold eight places of one dimension: a lane loads the same EPL dimensions of those eight places and pairs the halves
+//    with one v_perm per four bytes, row m of the instruction standing for dimension m*EPL + j in the j-th of EPL products.
+//  - Keys of the next tile are requested when this tile's scores are formed, values when its output is: two kinds of
+//    loads of a tile are in flight while the other kind is used, and the wavefronts of the CU hide the rest.
 #include "attention_internal.h"
 
 namespace moesys {
 namespace {
 
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int WAVES = 4;
+constexpr int HEADS = 16;  // query heads of a tile
+constexpr int TARGET_WORKGROUPS = 1024;
+constexpr int LEAST_PLACES = 256;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+// Rows of places that are not there and dimensions beyond head_dim are read from here: no load leaves the caller's rows, and what
+// lies in places that are not kept reaches no product.
+__device__ const u32x4 ZEROS[MOE_MAX_HEAD_DIM * 4 / 16] = {};
+
 struct DecodeArgs {
-  const void *k, *v, *q;
-  void* out;
+  const char *k, *v, *q;
+  char* out;
   float* lse;
   const int32_t *table, *lens;
   const float* slopes;
-  int64_t n_pages, page_stride, token_stride, head_stride, q_token, q_head, o_token, o_head;
-  int32_t page_size, table_width, hq, hkv, D, window;
-  float scale, cap;
+  float* part_o;   // [chunk*items][rows][D]
+  f32x2* part_ml;  // [chunk*items][rows]
+  int2* plan;      // [sequence]: first chunk, chunks
+  int64_t n_pages, page_stride, token_stride, head_stride, q_token, q_head, o_token, o_head;  // bytes
+  PageDivisor page;
+  int32_t page_size, table_width, n_seqs, hq, hkv, G, rows, items, D, window, least;
+  float scale, cap, inv_cap;
 };
 
-template <typename X> __device__ __forceinline__ float load(const X* p);
-template <> __device__ __forceinline__ float load<float>(const float* p) { return *p; }
-template <> __device__ __forceinline__ float load<uint16_t>(const uint16_t* p) { return bf16_to_float(*p); }
-__device__ __forceinline__ void store(float* p, float v) { *p = v; }
-__device__ __forceinline__ void store(uint16_t* p, float v) { *p = (uint16_t)float_to_bf16(v); }
+template <typename X, int DP> struct Shape;
+template <int DP> struct Shape<__bf16, DP> {
+  static constexpr int SUB = 2, EPL = DP < 128 ? 4 : 8, KSTEPS = DP / 32;
+};
+template <int DP> struct Shape<float, DP> {
+  static constexpr int SUB = 1, EPL = 4, KSTEPS = DP / 16;
+};
+
+template <int BYTES> struct Words;
+template <> struct Words<8> { typedef u32x2 type; };
+template <> struct Words<16> { typedef u32x4 type; };
+
+struct Chunk {
+  int b, j, n, first;  // sequence, which of its n chunks; the sequence's first chunk
+};
+
+__device__ __forceinline__ int tiles_of(const DecodeArgs& a, int b, int tile) {
+  const int n = kept_length(a.lens[b], a.table_width * a.page_size);
+  return kept_tiles(n, first_place(n, a.window), tile);
+}
+
+// Chunk number `pos` of the batch; every wavefront finds it by itself.  False: there are fewer chunks.
+__device__ __forceinline__ bool find_chunk(const DecodeArgs& a, int tile, int pos, Chunk* out) {
+  const int lane = threadIdx.x & 63;
+  int64_t total = 0;
+  for (int s = lane; s < a.n_seqs; s += 64) total += tiles_of(a, s, tile);
+#pragma unroll
+  for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d, 64);
+  const int c = chunk_tiles(total, a.items, TARGET_WORKGROUPS, a.least);
+  int before = 0;
+  for (int s = 0; s < a.n_seqs; s += 64) {
+    const int n = s + lane < a.n_seqs ? chunk_count(tiles_of(a, s + lane, tile), c) : 0;
+    int upto = n;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int other = __shfl_up(upto, d, 64);
+      if (lane >= d) upto += other;
+    }
+    const unsigned long long beyond = __ballot(before + upto > pos);
+    if (beyond) {
+      const int who = __ffsll(beyond) - 1;
+      out->b = s + who;
+      out->n = __builtin_amdgcn_readlane(n, who);
+      out->first = before + __builtin_amdgcn_readlane(upto, who) - out->n;
+      out->j = pos - out->first;
+      return true;
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
+  }
+  return false;
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const bf16x2 v = {(__bf16)lo, (__bf16)hi};
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+// Four finished elements of a head; the first four bring the head's lse along.
+template <typename X>
+__device__ __forceinline__ void store_row(const DecodeArgs& a, int b, int h, int d, f32x4 y, float sum, float top) {
+  if (sum == 0.f) y = f32x4{0.f, 0.f, 0.f, 0.f};
+  else y *= 1.f / sum;
+  char* p = a.out + (int64_t)b * a.o_token + (int64_t)h * a.o_head + d * sizeof(X);
+  if constexpr (sizeof(X) == 2) *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+  else *reinterpret_cast<f32x4*>(p) = y;
+  if (a.lse && d == 0) a.lse[(int64_t)b * a.hq + h] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
+}
+
+// One (sequence, kv head, tile of query heads, chunk of places) per workgroup; its wavefronts take the chunk's tiles in turn.
+// FULL: head_dim is DP, no lane's dimensions lie beyond it.
+template <typename X, int DP, bool FULL>
+__global__ __launch_bounds__(64 * WAVES) void decode_kernel(DecodeArgs a) {
+  using S = Shape<X, DP>;
+  constexpr bool BF16 = sizeof(X) == 2;
+  constexpr int SUB = S::SUB, TILE = 16 * SUB, EPL = S::EPL, KSTEPS = S::KSTEPS, NV = 4 * SUB, BD = 16 * EPL, NBLK = DP / BD, PITCH = BD + 4;
+  constexpr uint32_t EVERY = (uint32_t)((1ull << TILE) - 1);
+  using VWord = typename Words<EPL * sizeof(X)>::type;
+  extern __shared__ __attribute__((aligned(16))) float o_lds[];  // [WAVES][rows][PITCH]
+  __shared__ uint64_t row_at[WAVES][2][TILE];
+  __shared__ f32x2 ml_lds[WAVES][HEADS];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int m16 = lane & 15, g = lane >> 4;
+  const int item = blockIdx.x % a.items, hk = item % a.hkv, ht = item / a.hkv;
+  Chunk ch;
+  if (!find_chunk(a, TILE, blockIdx.x / a.items, &ch)) return;
+  const int n = kept_length(a.lens[ch.b], a.table_width * a.page_size), first = first_place(n, a.window);
+  const int tile0 = first / TILE, tiles = kept_tiles(n, first, TILE);
+  const int t_end = tile0 + chunk_begin(tiles, ch.n, ch.j + 1);
+  int t = tile0 + chunk_begin(tiles, ch.n, ch.j) + wave;
+  const int my_heads = a.G - ht * HEADS < HEADS ? a.G - ht * HEADS : HEADS;
+  if (threadIdx.x == 0 && item == 0 && ch.j == 0) a.plan[ch.b] = make_int2(ch.first, ch.n);
+
+  const char* zeros = reinterpret_cast<const char*>(ZEROS);
+  const char* base = (lane < 32 ? a.k : a.v) + hk * a.head_stride;  // lanes 0-31 place the keys' rows, the others the values'
+  const int32_t* table = a.table + (int64_t)ch.b * a.table_width;
+  const int tp = lane & (TILE - 1);
+
+  // the page of this lane's place of tile tt; no page for places outside the kept ones
+  auto page_of = [&](int tt) {
+    const int p = tt * TILE + tp;
+    return tt < t_end && p >= first && p < n ? table[a.page.quotient(p)] : -1;
+  };
+  // rows of tile tt into LDS; returns which places are kept
+  auto place_rows = [&](int tt, int entry) {
+    const int p = tt * TILE + tp, page = valid_page(entry, a.n_pages);
+    const int slot = p - a.page.quotient(p) * a.page_size;
+    const char* row = page >= 0 ? base + page * a.page_stride + slot * a.token_stride : zeros;
+    if ((lane & 31) < TILE) row_at[wave][lane >> 5][tp] = reinterpret_cast<uint64_t>(row);
+    const uint32_t kept = (uint32_t)__ballot(page >= 0) & EVERY;
+    asm volatile("" ::: "memory");  // (a wavefront's LDS operations execute in order)
+    return kept;
+  };
+
+  u32x4 kr[SUB][KSTEPS];
+  VWord vr[NV][NBLK];
+  auto load_keys = [&]() {
+#pragma unroll
+    for (int st = 0; st < SUB; ++st) {
+      const char* row = reinterpret_cast<const char*>(row_at[wave][0][st * 16 + m16]) + g * 16;
+#pragma unroll
+      for (int s = 0; s < KSTEPS; ++s) {
+        const char* p = row + s * 64;
+        if (!FULL && s * 64 + g * 16 >= a.D * (int)sizeof(X)) p = zeros;
+        kr[st][s] = *reinterpret_cast<const u32x4*>(p);
+      }
+    }
+  };
+  auto load_values = [&]() {
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      const char* row = reinterpret_cast<const char*>(row_at[wave][1][u / 4 * 16 + g * 4 + u % 4]) + m16 * (EPL * sizeof(X));
+#pragma unroll
+      for (int blk = 0; blk < NBLK; ++blk) {
+        const char* p = row + blk * (BD * sizeof(X));
+        if (!FULL && (blk * 16 + m16) * EPL >= a.D) p = zeros;
+        vr[u][blk] = *reinterpret_cast<const VWord*>(p);
+      }
+    }
+  };
+
+  int entry = page_of(t), entry_next = page_of(t + WAVES);
+  u32x4 qr[KSTEPS];
+  {
+    const bool have = m16 < my_heads;
+    const char* row = a.q + (int64_t)ch.b * a.q_token + (int64_t)(hk * a.G + ht * HEADS + m16) * a.q_head + g * 16;
+#pragma unroll
+    for (int s = 0; s < KSTEPS; ++s) qr[s] = *reinterpret_cast<const u32x4*>(have && (s * 64 + g * 16) < a.D * (int)sizeof(X) ? row + s * 64 : zeros);
+  }
+  const float slope = a.slopes && m16 < my_heads ? a.slopes[hk * a.G + ht * HEADS + m16] : 0.f;
+  const bool plain = a.cap == 0.f && !a.slopes;
+  const float scale2 = a.scale * LOG2E;
+
+  float m = -INFINITY, mref = 0.f, l = 0.f;
+  f32x4 o[NBLK][EPL];
+#pragma unroll
+  for (int blk = 0; blk < NBLK; ++blk)
+#pragma unroll
+    for (int j = 0; j < EPL; ++j) o[blk][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  uint32_t kept = 0;
+  if (t < t_end) {
+    kept = place_rows(t, entry);
+    load_keys();
+    load_values();
+  }
+  for (; t < t_end; t += WAVES) {
+    const uint32_t here = kept;
+    entry = entry_next;
+    entry_next = page_of(t + 2 * WAVES);
+    f32x4 z[SUB];
+#pragma unroll
+    for (int st = 0; st < SUB; ++st) {
+      z[st] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < KSTEPS; ++s) {
+        if constexpr (BF16) {
+          z[st] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[st][s]), __builtin_bit_cast(bf16x8, qr[s]), z[st], 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            z[st] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[st][s][e]), __uint_as_float(qr[s][e]), z[st], 0, 0, 0);
+        }
+      }
+    }
+    const bool more = t + WAVES < t_end;
+    if (more) {
+      kept = place_rows(t + WAVES, entry);
+      load_keys();
+    }
+    // scores in units of log 2
+    if (plain) {
+#pragma unroll
+      for (int st = 0; st < SUB; ++st) z[st] *= scale2;
+    } else {
+#pragma unroll
+      for (int st = 0; st < SUB; ++st)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float s = z[st][i] * a.scale;
+          if (a.cap > 0.f) s = a.cap * tanhf(s * a.inv_cap);
+          s -= slope * (float)(n - 1 - (t * TILE + st * 16 + g * 4 + i));
+          z[st][i] = s * LOG2E;
+        }
+    }
+    if (here != EVERY) {
+#pragma unroll
+      for (int st = 0; st < SUB; ++st)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (!((here >> (st * 16 + g * 4 + i)) & 1)) z[st][i] = -INFINITY;
+    }
+    float top = z[0][0];
+#pragma unroll
+    for (int st = 0; st < SUB; ++st)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = fmaxf(top, z[st][i]);
+    // The maximum moves only when some score passes it by a factor of 2^8: until then the weights grow to at most that, which
+    // float32 sums do not mind, and the four lanes of a head need not exchange theirs.
+    if (__any(top > m + 8.f)) {
+      top = fmaxf(top, __shfl_xor(top, 16, 64));
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      const float now = fmaxf(m, top), f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - now);
+      m = now;
+      mref = now == -INFINITY ? 0.f : now;
+      l *= f;
+#pragma unroll
+      for (int blk = 0; blk < NBLK; ++blk)
+#pragma unroll
+        for (int j = 0; j < EPL; ++j) o[blk][j] *= f;
+    }
+#pragma unroll
+    for (int st = 0; st < SUB; ++st)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        z[st][i] = __builtin_amdgcn_exp2f(z[st][i] - mref);
+        l += z[st][i];
+      }
+    if constexpr (BF16) {
+      // A weight enters as the sum of two bfloat16 numbers, 16 bits of mantissa: one alone would add half of the output's own
+      // rounding to its error, and the matrix units are idle most of the time.
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float p0 = z[i / 2][i % 2 * 2], p1 = z[i / 2][i % 2 * 2 + 1];
+        hi[i] = pack_bf16(p0, p1);
+        lo[i] = pack_bf16(p0 - __uint_as_float(hi[i] << 16), p1 - __uint_as_float(hi[i] & 0xffff0000u));
+      }
+      const bf16x8 ph = __builtin_bit_cast(bf16x8, (u32x4{hi[0], hi[1], hi[2], hi[3]}));
+      const bf16x8 pl = __builtin_bit_cast(bf16x8, (u32x4{lo[0], lo[1], lo[2], lo[3]}));
+#pragma unroll
+      for (int blk = 0; blk < NBLK; ++blk)
+#pragma unroll
+        for (int j = 0; j < EPL; ++j) {
+          u32x4 w;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            w[i] = __builtin_amdgcn_perm(vr[2 * i + 1][blk][j / 2], vr[2 * i][blk][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+          const bf16x8 vt = __builtin_bit_cast(bf16x8, w);
+          o[blk][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, ph, o[blk][j], 0, 0, 0);
+          o[blk][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pl, o[blk][j], 0, 0, 0);
+        }
+    } else {
+#pragma unroll
+      for (int blk = 0; blk < NBLK; ++blk)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < EPL; ++j)
+            o[blk][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[i][blk][j]), z[0][i], o[blk][j], 0, 0, 0);
+    }
+    if (more) load_values();
+  }
+
+  // the wavefronts' parts: common maximum, then the sum through LDS
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  if (g == 0) ml_lds[wave][m16] = f32x2{m, l};
+  __syncthreads();
+  auto joined_max = [&](int head) {
+    float top = ml_lds[0][head][0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) top = fmaxf(top, ml_lds[w][head][0]);
+    return top;
+  };
+  auto part_weight = [&](int w, int head, float top) { return top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml_lds[w][head][0] - top); };
+  const float f = m16 < my_heads ? part_weight(wave, m16, joined_max(m16)) : 0.f;
+  const int d = threadIdx.x % (BD / 4) * 4;
+#pragma unroll
+  for (int blk = 0; blk < NBLK; ++blk) {
+    if (blk) __syncthreads();
+    if (m16 < my_heads) {
+      float* row = o_lds + (wave * a.rows + m16) * PITCH;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < EPL; j += 4)
+          *reinterpret_cast<f32x4*>(row + (g * 4 + i) * EPL + j) =
+              f32x4{o[blk][j][i] * f, o[blk][j + 1][i] * f, o[blk][j + 2][i] * f, o[blk][j + 3][i] * f};
+    }
+    __syncthreads();
+    const int dim = blk * BD + d;
+    for (int r = threadIdx.x / (BD / 4); r < my_heads; r += 64 * WAVES / (BD / 4)) {
+      const float top = joined_max(r);
+      float sum = 0.f;
+      f32x4 y{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        sum += ml_lds[w][r][1] * part_weight(w, r, top);
+        y += *reinterpret_cast<const f32x4*>(o_lds + (w * a.rows + r) * PITCH + d);
+      }
+      if (!FULL && dim >= a.D) continue;
+      const int h = hk * a.G + ht * HEADS + r;
+      if (ch.n == 1) {
+        store_row<X>(a, ch.b, h, dim, y, sum, top);
+      } else {
+        const int64_t at = (int64_t)blockIdx.x * a.rows + r;
+        *reinterpret_cast<f32x4*>(a.part_o + at * a.D + dim) = y;
+        if (dim == 0) a.part_ml[at] = f32x2{top, sum};
+      }
+    }
+  }
+}
+
+// Joins the chunks of one (sequence, query head) in their order; sequences of one chunk are complete already.
+constexpr int JOIN_THREADS = 256;
+template <typename X>
+__global__ __launch_bounds__(JOIN_THREADS) void join_kernel(DecodeArgs a) {
+  extern __shared__ __attribute__((aligned(16))) float weight[];  // one per chunk
+  __shared__ float red[JOIN_THREADS / 64];
+  __shared__ f32x4 sums[JOIN_THREADS];
+  const int b = blockIdx.x / a.hq, h = blockIdx.x % a.hq;
+  const int2 plan = a.plan[b];
+  if (plan.y <= 1) return;
+  const int hk = h / a.G, r = h % a.G % HEADS, item = h % a.G / HEADS * a.hkv + hk;
+  auto at = [&](int j) { return ((int64_t)(plan.x + j) * a.items + item) * a.rows + r; };
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  float top = -INFINITY;
+  for (int j = tid; j < plan.y; j += JOIN_THREADS) top = fmaxf(top, a.part_ml[at(j)][0]);
+#pragma unroll
+  for (int s = 32; s; s >>= 1) top = fmaxf(top, __shfl_xor(top, s, 64));
+  if (lane == 0) red[wave] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < JOIN_THREADS / 64; ++w) top = fmaxf(top, red[w]);
+  __syncthreads();
+  float sum = 0.f;
+  for (int j = tid; j < plan.y; j += JOIN_THREADS) {
+    const f32x2 ml = a.part_ml[at(j)];
+    const float f = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[0] - top);
+    weight[j] = f;
+    sum += f * ml[1];
+  }
+#pragma unroll
+  for (int s = 32; s; s >>= 1) sum += __shfl_xor(sum, s, 64);
+  if (lane == 0) red[wave] = sum;
+  __syncthreads();
+  sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < JOIN_THREADS / 64; ++w) sum += red[w];
+  const int across = a.D <= 64 ? 16 : a.D <= 128 ? 32 : 64, d = tid % across * 4, groups = JOIN_THREADS / across;
+  f32x4 y{0.f, 0.f, 0.f, 0.f};
+  if (d < a.D)
+    for (int j = tid / across; j < plan.y; j += groups) y += weight[j] * *reinterpret_cast<const f32x4*>(a.part_o + at(j) * a.D + d);
+  sums[tid] = y;
+  __syncthreads();
+  if (tid >= across || d >= a.D) return;
+  for (int i = 1; i < groups; ++i) y += sums[tid + i * across];
+  store_row<X>(a, b, h, d, y, sum, top);
+}
+
+// The split of a call: what its grid, its workspace and its kernels agree on.
+struct Split {
+  int rows, items, least;
+  int64_t chunks, tiles;  // most chunks of a batch, most tiles of a sequence
+  size_t ml, o, total;    // bytes: offsets of the parts (the plan lies in front)
+};
+
+Split split_of(const moe_kv_cache* c, int32_t n_q_heads) {
+  Split s;
+  const int G = n_q_heads / c->n_kv_heads, tile = c->dtype == MOE_BF16 ? 32 : 16;
+  s.rows = G < HEADS ? G : HEADS;
+  s.items = c->n_kv_heads * ((G + HEADS - 1) / HEADS);
+  s.least = LEAST_PLACES / tile;
+  s.tiles = ((int64_t)c->table_width * c->page_size + tile - 1) / tile;
+  s.chunks = most_chunks(c->n_seqs, s.items, TARGET_WORKGROUPS, s.least, s.tiles);
+  s.ml = align_up((size_t)c->n_seqs * sizeof(int2), 256);
+  s.o = s.ml + align_up((size_t)s.chunks * s.items * s.rows * sizeof(f32x2), 256);
+  s.total = s.o + align_up((size_t)s.chunks * s.items * s.rows * c->head_dim * sizeof(float), 256);
+  if (s.total < 256) s.total = 256;
+  return s;
+}
+
+template <typename X, int DP>
+void launch(const DecodeArgs& a, unsigned grid, hipStream_t s) {
+  const size_t lds = (size_t)WAVES * a.rows * (16 * Shape<X, DP>::EPL + 4) * sizeof(float);
+  if (a.D == DP) hipLaunchKernelGGL((decode_kernel<X, DP, true>), dim3(grid), dim3(64 * WAVES), lds, s, a);
+  else hipLaunchKernelGGL((decode_kernel<X, DP, false>), dim3(grid), dim3(64 * WAVES), lds, s, a);
+}
 
 template <typename X>
-__global__ __launch_bounds__(64) void decode_kernel(DecodeArgs a) {
-  const int b = blockIdx.x, h = blockIdx.y, hk = h / (a.hq / a.hkv), lane = threadIdx.x;
-  const int n = kept_length(a.lens[b], a.table_width * a.page_size);
-  float q[4], o[4] = {0.f, 0.f, 0.f, 0.f}, m = -INFINITY, l = 0.f;
-  for (int i = 0; i < 4; ++i) q[i] = lane + 64 * i < a.D ? load((const X*)a.q + b * a.q_token + h * a.q_head + lane + 64 * i) : 0.f;
-  const float slope = a.slopes ? a.slopes[h] : 0.f;
-  for (int j = first_place(n, a.window); j < n; ++j) {
-    const int page = valid_page(a.table[(int64_t)b * a.table_width + j / a.page_size], a.n_pages);
-    if (page < 0) continue;
-    const int64_t at = page * a.page_stride + (j % a.page_size) * a.token_stride + hk * a.head_stride;
-    float z = 0.f;
-    for (int i = 0; i < 4; ++i)
-      if (lane + 64 * i < a.D) z = fmaf(q[i], load((const X*)a.k + at + lane + 64 * i), z);
-    for (int s = 32; s; s >>= 1) z += __shfl_xor(z, s, 64);
-    z *= a.scale;
-    if (a.cap > 0.f) z = a.cap * tanhf(z / a.cap);
-    z -= slope * (float)(n - 1 - j);
-    const float top = fmaxf(m, z);
-    if (top == -INFINITY) continue;
-    const float w = expf(z - top), old = expf(m - top);
-    m = top;
-    l = l * old + w;
-    for (int i = 0; i < 4; ++i)
-      if (lane + 64 * i < a.D) o[i] = o[i] * old + w * load((const X*)a.v + at + lane + 64 * i);
-  }
-  for (int i = 0; i < 4; ++i)
-    if (lane + 64 * i < a.D) store((X*)a.out + b * a.o_token + h * a.o_head + lane + 64 * i, l > 0.f ? o[i] / l : l == 0.f ? 0.f : l);
-  if (a.lse && lane == 0) a.lse[(int64_t)b * a.hq + h] = logf(l) + m;
+int32_t launch_decode(const DecodeArgs& a, const Split& sp, hipStream_t s) {
+  const unsigned grid = (unsigned)(sp.chunks * sp.items);
+  if (a.D <= 64) launch<X, 64>(a, grid, s);
+  else if (a.D <= 128) launch<X, 128>(a, grid, s);
+  else launch<X, 256>(a, grid, s);
+  int32_t st = check_hip(hipGetLastError(), "attention launch");
+  if (st != MOE_OK || sp.tiles <= sp.least) return st;  // (no sequence can have two chunks)
+  const size_t weights = (size_t)(TARGET_WORKGROUPS / sp.items + 2) * sizeof(float);
+  hipLaunchKernelGGL(join_kernel<X>, dim3((unsigned)(a.n_seqs * a.hq)), dim3(JOIN_THREADS), weights, s, a);
+  return check_hip(hipGetLastError(), "attention join launch");
 }
 
 }  // namespace
@@ -66,7 +475,7 @@ extern "C" size_t moe_attention_decode_workspace_bytes(const moe_kv_cache* c, in
     fail(MOE_ERR_INVALID_ARG, "n_q_heads=%d must be a multiple of n_kv_heads=%d in 1..%d", n_q_heads, c->n_kv_heads, MOE_MAX_HEADS);
     return 0;
   }
-  return 256;
+  return split_of(c, n_q_heads).total;
 }
 
 extern "C" int32_t moe_attention_decode(const moe_kv_cache* c, int32_t n_q_heads, const moe_head_rows* q, const int32_t* seq_lens,
@@ -82,18 +491,48 @@ extern "C" int32_t moe_attention_decode(const moe_kv_cache* c, int32_t n_q_heads
   if (opt->window < 0) return fail(MOE_ERR_INVALID_ARG, "moe_attention_decode: window=%d is negative", opt->window);
   if (c->n_seqs == 0) return MOE_OK;
   if (!q || !q->data || !out || !out->data || !seq_lens) return fail(MOE_ERR_INVALID_ARG, "moe_attention_decode: q, out and seq_lens must be non-NULL");
-  const size_t es = elem_size(c->dtype);
+  const int64_t es = (int64_t)elem_size(c->dtype);
   if (!rows_aligned(q, es) || !rows_aligned(out, es))
     return fail(MOE_ERR_INVALID_ARG, "moe_attention_decode: pointers and strides of q and out must be multiples of 16 bytes");
+  const Split sp = split_of(c, n_q_heads);
+  if (sp.chunks * sp.items > INT32_MAX || (int64_t)c->n_seqs * n_q_heads > INT32_MAX)
+    return fail(MOE_ERR_UNSUPPORTED, "moe_attention_decode: %d sequences of %d query heads are too many for one call", c->n_seqs, n_q_heads);
   if (!ws || ((uintptr_t)ws & 255) || ws_bytes < need)
     return fail(MOE_ERR_WORKSPACE, "moe_attention_decode: workspace NULL, misaligned or smaller than %zu bytes", need);
-  const DecodeArgs a{c->k, c->v, q->data, out->data, lse, c->page_table, seq_lens, opt->slopes, c->n_pages, c->page_stride, c->token_stride,
-                     c->head_stride, q->token_stride, q->head_stride, out->token_stride, out->head_stride, c->page_size, c->table_width,
-                     n_q_heads, c->n_kv_heads, c->head_dim, opt->window, opt->scale, opt->softcap};
-  dim3 grid(c->n_seqs, n_q_heads);
-  if (c->dtype == MOE_BF16)
-    hipLaunchKernelGGL(decode_kernel<uint16_t>, grid, dim3(64), 0, (hipStream_t)stream, a);
-  else
-    hipLaunchKernelGGL(decode_kernel<float>, grid, dim3(64), 0, (hipStream_t)stream, a);
-  return check_hip(hipGetLastError(), "attention launch");
+  DecodeArgs a{};
+  a.k = (const char*)c->k;
+  a.v = (const char*)c->v;
+  a.q = (const char*)q->data;
+  a.out = (char*)out->data;
+  a.lse = lse;
+  a.table = c->page_table;
+  a.lens = seq_lens;
+  a.slopes = opt->slopes;
+  a.plan = (int2*)ws;
+  a.part_ml = (f32x2*)((char*)ws + sp.ml);
+  a.part_o = (float*)((char*)ws + sp.o);
+  a.n_pages = c->n_pages;
+  a.page_stride = c->page_stride * es;
+  a.token_stride = c->token_stride * es;
+  a.head_stride = c->head_stride * es;
+  a.q_token = q->token_stride * es;
+  a.q_head = q->head_stride * es;
+  a.o_token = out->token_stride * es;
+  a.o_head = out->head_stride * es;
+  a.page = page_divisor(c->page_size);
+  a.page_size = c->page_size;
+  a.table_width = c->table_width;
+  a.n_seqs = c->n_seqs;
+  a.hq = n_q_heads;
+  a.hkv = c->n_kv_heads;
+  a.G = n_q_heads / c->n_kv_heads;
+  a.rows = sp.rows;
+  a.items = sp.items;
+  a.D = c->head_dim;
+  a.window = opt->window;
+  a.least = sp.least;
+  a.scale = opt->scale;
+  a.cap = opt->softcap;
+  a.inv_cap = opt->softcap > 0.f ? 1.f / opt->softcap : 0.f;
+  return c->dtype == MOE_BF16 ? launch_decode<__bf16>(a, sp, (hipStream_t)stream) : launch_decode<float>(a, sp, (hipStream_t)stream);
 }

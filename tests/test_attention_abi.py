@@ -181,3 +181,38 @@ def test_places_on_the_host(tmp_path):
   assert(first_place(10, 0) == 0 && first_place(10, 10) == 0 && first_place(10, 3) == 7 && first_place(0, 3) == 0 && first_place(2147483647, 1) == 2147483646);
   assert(valid_page(-1, 5) == -1 && valid_page(5, 5) == -1 && valid_page(4, 5) == 4 && valid_page(0, 0) == -1 && valid_page(2147483647, 2147483647) == -1);
 }""")
+
+
+def test_pages_and_chunks_on_the_host(tmp_path):
+    """Page numbers by multiplication equal division; the chunks of a sequence cover its tiles once, in order; no batch has more
+    than the grid and the workspace are made for."""
+    compiled(tmp_path, """
+unsigned long long seed = 1;
+unsigned next() { seed = seed * 6364136223846793005ull + 1442695040888963407ull; return (unsigned)(seed >> 33); }
+int main() {
+  for (int d : {1, 2, 3, 5, 7, 16, 20, 100, 1000, 65535, 65536, 65537, 1000003, 1 << 30, (1 << 30) + 1, 2147483646, 2147483647}) {
+    const PageDivisor q = page_divisor(d);
+    for (int i = 0; i < 20000; ++i) { const int p = (int)(next() & 2147483647u); assert(q.quotient(p) == p / d); }
+    for (long long k = 0; k < 50; ++k)
+      for (int e = -1; e < 2; ++e) { const long long p = k * d + e; if (p >= 0 && p < 2147483648ll) assert(q.quotient((int)p) == (int)(p / d)); }
+    for (int e = 0; e < 100; ++e) assert(q.quotient(2147483647 - e) == (2147483647 - e) / d);
+  }
+  assert(kept_tiles(0, 0, 32) == 0 && kept_tiles(1, 0, 32) == 1 && kept_tiles(32, 0, 32) == 1 && kept_tiles(33, 0, 32) == 2);
+  assert(kept_tiles(33, 31, 32) == 2 && kept_tiles(33, 32, 32) == 1 && kept_tiles(2147483647, 0, 32) == 67108864);
+  for (int round = 0; round < 3000; ++round) {
+    const int items = 1 + next() % 300, target = 1 + next() % 2048, least = 1 + next() % 20, S = 1 + next() % 40;
+    const long long cap = 1 + next() % (round % 3 ? 200 : 100000);
+    std::vector<int> tiles(S);
+    long long total = 0, chunks = 0;
+    for (int& t : tiles) { t = next() % 5 ? (int)(next() % (cap + 1)) : 0; total += t; }
+    const int c = chunk_tiles(total, items, target, least);
+    for (int t : tiles) {
+      const int n = chunk_count(t, c);
+      chunks += n;
+      assert(n >= 1 && n <= target / items + 1 && chunk_begin(t, n, 0) == 0 && chunk_begin(t, n, n) == t);
+      for (int j = 0; j < n; ++j) { const int size = chunk_begin(t, n, j + 1) - chunk_begin(t, n, j); assert(size <= c && (size > 0 || t == 0)); }
+    }
+    assert(chunks <= most_chunks(S, items, target, least, cap));
+    if (cap <= least) assert(chunks == S);
+  }
+}""")
