@@ -65,7 +65,7 @@ def _dtype(t) -> int:
 
 def _rows(t, what: str, shape, dtype) -> _HeadRows:
     """[tokens, heads, head_dim] as the library takes it, checked against what the call says it holds."""
-    if tuple(t.shape) != shape:
+    if t.shape != shape:
         raise ValueError(f"{what} has shape {tuple(t.shape)}, the call needs {shape}")
     if t.dtype != dtype:
         raise ValueError(f"{what} is {t.dtype}, the call needs {dtype}")
@@ -84,16 +84,26 @@ def _ints(t, what: str, *shapes) -> Optional[int]:
     return t.data_ptr()
 
 
-def _on_device(*tensors) -> None:
-    first = None
+def _on_device(*tensors) -> int:
+    """The one CUDA device that all of the tensors are on."""
+    device = -1
     for t in tensors:
         if t is None:
             continue
-        if not t.is_cuda:
+        d = t.get_device()
+        if d < 0:
             raise ValueError("device tensors are needed")
-        first = t.device if first is None else first
-        if t.device != first:
-            raise ValueError(f"tensors on {first} and {t.device}")
+        if device < 0:
+            device = d
+        elif d != device:
+            raise ValueError(f"tensors on CUDA devices {device} and {d}")
+    return device
+
+
+def _stream(stream, device: int) -> Optional[int]:
+    """The given stream, or the device's current one; the raw handle spares a decoded token's calls the 2.7 us that building
+    torch's stream object takes, as much as all their other checks together."""
+    return (torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream) or None
 
 
 class Rotary:
@@ -146,12 +156,12 @@ class KVCache:
 def moe_rotary(rotary: Rotary, x, positions, out, inverse: bool = False, stream=None):
     """out <- x [T, heads, head_dim] rotated by positions [axes, T] (int32); ``inverse``: back, or the gradient."""
     T, H, D = x.shape
-    _on_device(x, positions, out, rotary.freqs)
+    device = _on_device(x, positions, out, rotary.freqs)
     if D != rotary.head_dim:
         raise ValueError(f"x has heads of {D}, the rotary positions are for {rotary.head_dim}")
     xr, outr = _rows(x, "x", (T, H, D), x.dtype), _rows(out, "out", (T, H, D), x.dtype)
     pos = _ints(positions, "positions", (rotary.n_axes, T), *([(T,)] if rotary.n_axes == 1 else []))
-    B._check(lib().moe_rotary(C.byref(rotary.c), _dtype(x), T, H, C.byref(xr), pos, C.byref(outr), int(bool(inverse)), B._stream(stream)), "moe_rotary")
+    B._check(lib().moe_rotary(C.byref(rotary.c), _dtype(x), T, H, C.byref(xr), pos, C.byref(outr), int(bool(inverse)), _stream(stream, device)), "moe_rotary")
 
 
 def moe_kv_append(cache: KVCache, k, v, cache_pos, token_seq=None, rotary: Optional[Rotary] = None, positions=None, q=None, q_out=None,
@@ -159,7 +169,7 @@ def moe_kv_append(cache: KVCache, k, v, cache_pos, token_seq=None, rotary: Optio
     """Keys and values [T, kv_heads, head_dim] of new tokens into their places of the cache, keys rotated; queries
     [T, heads, head_dim] rotated into q_out."""
     T = k.shape[0]
-    _on_device(k, v, cache_pos, token_seq, positions, q, q_out, cache.k, rotary.freqs if rotary is not None else None)
+    device = _on_device(k, v, cache_pos, token_seq, positions, q, q_out, cache.k, rotary.freqs if rotary is not None else None)
     kv = (T, cache.n_kv_heads, cache.head_dim)
     kr, vr = _rows(k, "k", kv, cache.dtype), _rows(v, "v", kv, cache.dtype)
     qr = qo = None
@@ -173,7 +183,7 @@ def moe_kv_append(cache: KVCache, k, v, cache_pos, token_seq=None, rotary: Optio
     B._check(lib().moe_kv_append(
         C.byref(cache.c), T, C.byref(kr), C.byref(vr), _ints(token_seq, "token_seq", (T,)), _ints(cache_pos, "cache_pos", (T,)),
         C.byref(rotary.c) if rotary is not None else None, _ints(positions, "positions", (axes, T), *([(T,)] if axes == 1 else [])), hq,
-        C.byref(qr) if qr is not None else None, C.byref(qo) if qo is not None else None, B._stream(stream)), "moe_kv_append")
+        C.byref(qr) if qr is not None else None, C.byref(qo) if qo is not None else None, _stream(stream, device)), "moe_kv_append")
 
 
 def moe_attention_decode_workspace_bytes(cache: KVCache, n_q_heads: int) -> int:
@@ -188,7 +198,7 @@ def moe_attention_decode(cache: KVCache, q, seq_lens, out, ws, scale: Optional[f
     """Attention of one new token per sequence: q, out [sequences, heads, head_dim], seq_lens int32 [sequences] (the new token
     counted), slopes float32 [heads] (optional), lse float32 [sequences, heads] (optional output)."""
     S, H, D = cache.n_seqs, q.shape[1], cache.head_dim
-    _on_device(q, seq_lens, out, ws, slopes, lse, cache.k)
+    device = _on_device(q, seq_lens, out, ws, slopes, lse, cache.k)
     qr, outr = _rows(q, "q", (S, H, D), cache.dtype), _rows(out, "out", (S, H, D), cache.dtype)
     for t, what, shape in ((slopes, "slopes", (H,)), (lse, "lse", (S, H))):
         if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous()):
@@ -198,4 +208,4 @@ def moe_attention_decode(cache: KVCache, q, seq_lens, out, ws, scale: Optional[f
     opt = _Options(D ** -0.5 if scale is None else scale, softcap, window, slopes.data_ptr() if slopes is not None else None)
     B._check(lib().moe_attention_decode(
         C.byref(cache.c), H, C.byref(qr), _ints(seq_lens, "seq_lens", (S,)), C.byref(opt), C.byref(outr), lse.data_ptr() if lse is not None else None,
-        ws.data_ptr(), ws.numel() * ws.element_size(), B._stream(stream)), "moe_attention_decode")
+        ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream, device)), "moe_attention_decode")
