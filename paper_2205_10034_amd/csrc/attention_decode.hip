@@ -15,6 +15,7 @@
 //  - Keys of the next tile are requested when this tile's scores are formed, values when its output is: two kinds of
 //    loads of a tile are in flight while the other kind is used, and the wavefronts of the CU hide the rest.
 #include "attention_internal.h"
+#include "wave_util.h"
 
 namespace moesys {
 namespace {
@@ -29,7 +30,6 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 constexpr int WAVES = 4;
 constexpr int HEADS = 16;  // query heads of a tile
 constexpr int TARGET_WORKGROUPS = 1024;
-constexpr int LEAST_PLACES = 256;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 // Rows of places that are not there and dimensions beyond head_dim are read from here: no load leaves the caller's rows, and what
@@ -47,7 +47,7 @@ struct DecodeArgs {
   int2* plan;      // [sequence]: first chunk, chunks
   int64_t n_pages, page_stride, token_stride, head_stride, q_token, q_head, o_token, o_head;  // bytes
   PageDivisor page;
-  int32_t page_size, table_width, n_seqs, hq, hkv, G, rows, items, D, window, least;
+  int32_t page_size, table_width, n_seqs, hq, hkv, G, rows, items, wave_heads, D, window, least;
   float scale, cap, inv_cap;
 };
 
@@ -73,13 +73,13 @@ __device__ __forceinline__ int tiles_of(const DecodeArgs& a, int b, int tile) {
 }
 
 // Chunk number `pos` of the batch; every wavefront finds it by itself.  False: there are fewer chunks.
-__device__ __forceinline__ bool find_chunk(const DecodeArgs& a, int tile, int pos, Chunk* out) {
+__device__ __forceinline__ bool find_chunk(const DecodeArgs& a, int tile, int groups, int pos, Chunk* out) {
   const int lane = threadIdx.x & 63;
   int64_t total = 0;
   for (int s = lane; s < a.n_seqs; s += 64) total += tiles_of(a, s, tile);
 #pragma unroll
   for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d, 64);
-  const int c = chunk_tiles(total, a.items, TARGET_WORKGROUPS, a.least);
+  const int c = chunk_tiles(total, groups, TARGET_WORKGROUPS, a.least);
   int before = 0;
   for (int s = 0; s < a.n_seqs; s += 64) {
     const int n = s + lane < a.n_seqs ? chunk_count(tiles_of(a, s + lane, tile), c) : 0;
@@ -108,6 +108,32 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, v);
 }
 
+// Addresses that come out of LDS are global ones: told so, the compiler reads them with loads that the waits for LDS do not wait for.
+template <bool NT, typename W>
+__device__ __forceinline__ W read(const char* p) {
+  const auto* at = (const __attribute__((address_space(1))) W*)(uintptr_t)p;
+  if constexpr (NT) return __builtin_nontemporal_load(at);
+  else return *at;
+}
+
+// acc + a b for 16 bytes of contraction index per lane and operand
+template <bool BF16>
+__device__ __forceinline__ f32x4 product(const u32x4& a, const u32x4& b, f32x4 acc) {
+  if constexpr (BF16) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[e]), __uint_as_float(b[e]), acc, 0, 0, 0);
+    return acc;
+  }
+}
+
+// What the lane 32 away holds.
+__device__ __forceinline__ float other_half(float x, int lane) {
+  const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(lane < 32 ? both[1] : both[0]);
+}
+
 // Four finished elements of a head; the first four bring the head's lse along.
 template <typename X>
 __device__ __forceinline__ void store_row(const DecodeArgs& a, int b, int h, int d, f32x4 y, float sum, float top) {
@@ -121,11 +147,11 @@ __device__ __forceinline__ void store_row(const DecodeArgs& a, int b, int h, int
 
 // One (sequence, kv head, tile of query heads, chunk of places) per workgroup; its wavefronts take the chunk's tiles in turn.
 // FULL: head_dim is DP, no lane's dimensions lie beyond it.
-template <typename X, int DP, bool FULL>
+template <typename X, int DP, bool FULL, bool NT>
 __global__ __launch_bounds__(64 * WAVES) void decode_kernel(DecodeArgs a) {
   using S = Shape<X, DP>;
   constexpr bool BF16 = sizeof(X) == 2;
-  constexpr int SUB = S::SUB, TILE = 16 * SUB, EPL = S::EPL, KSTEPS = S::KSTEPS, NV = 4 * SUB, BD = 16 * EPL, NBLK = DP / BD, PITCH = BD + 4;
+  constexpr int SUB = S::SUB, TILE = 16 * SUB, EPL = S::EPL, KSTEPS = S::KSTEPS, LINES = KSTEPS / 2, NV = 4 * SUB, BD = 16 * EPL, NBLK = DP / BD, PITCH = BD + 4;
   constexpr uint32_t EVERY = (uint32_t)((1ull << TILE) - 1);
   using VWord = typename Words<EPL * sizeof(X)>::type;
   extern __shared__ __attribute__((aligned(16))) float o_lds[];  // [WAVES][rows][PITCH]
@@ -133,14 +159,16 @@ __global__ __launch_bounds__(64 * WAVES) void decode_kernel(DecodeArgs a) {
   __shared__ f32x2 ml_lds[WAVES][HEADS];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int m16 = lane & 15, g = lane >> 4;
-  const int item = blockIdx.x % a.items, hk = item % a.hkv, ht = item / a.hkv;
+  const int m16 = lane & 15, g = lane >> 4, piece = (g + 4 * (m16 >> 3)) * 16;
+  // wavefronts of a workgroup: wave_heads neighbouring kv heads, `step` of them on the tiles of each in turn
+  const int groups = a.items / a.wave_heads, pos = blockIdx.x / groups, step = WAVES / a.wave_heads;
+  const int item = blockIdx.x % groups * a.wave_heads + wave % a.wave_heads, hk = item % a.hkv, ht = item / a.hkv;
   Chunk ch;
-  if (!find_chunk(a, TILE, blockIdx.x / a.items, &ch)) return;
+  if (!find_chunk(a, TILE, groups, pos, &ch)) return;
   const int n = kept_length(a.lens[ch.b], a.table_width * a.page_size), first = first_place(n, a.window);
   const int tile0 = first / TILE, tiles = kept_tiles(n, first, TILE);
   const int t_end = tile0 + chunk_begin(tiles, ch.n, ch.j + 1);
-  int t = tile0 + chunk_begin(tiles, ch.n, ch.j) + wave;
+  int t = tile0 + chunk_begin(tiles, ch.n, ch.j) + wave / a.wave_heads;
   const int my_heads = a.G - ht * HEADS < HEADS ? a.G - ht * HEADS : HEADS;
   if (threadIdx.x == 0 && item == 0 && ch.j == 0) a.plan[ch.b] = make_int2(ch.first, ch.n);
 
@@ -149,35 +177,41 @@ __global__ __launch_bounds__(64 * WAVES) void decode_kernel(DecodeArgs a) {
   const int32_t* table = a.table + (int64_t)ch.b * a.table_width;
   const int tp = lane & (TILE - 1);
 
-  // the page of this lane's place of tile tt; no page for places outside the kept ones
-  auto page_of = [&](int tt) {
+  // Nothing in the loop that loads is conditional: what a tile beyond the last one would load is ZEROS.  (Behind a branch the
+  // compiler waits for every load in flight before it uses the first.)
+  auto is_kept = [&](int tt) {
     const int p = tt * TILE + tp;
-    return tt < t_end && p >= first && p < n ? table[a.page.quotient(p)] : -1;
+    return tt < t_end && p >= first && p < n;
   };
+  // the table's entry for this lane's place of tile tt
+  auto entry_of = [&](int tt) { return table[is_kept(tt) ? a.page.quotient(tt * TILE + tp) : 0]; };
   // rows of tile tt into LDS; returns which places are kept
   auto place_rows = [&](int tt, int entry) {
-    const int p = tt * TILE + tp, page = valid_page(entry, a.n_pages);
+    const int p = tt * TILE + tp, page = is_kept(tt) ? valid_page(entry, a.n_pages) : -1;
     const int slot = p - a.page.quotient(p) * a.page_size;
     const char* row = page >= 0 ? base + page * a.page_stride + slot * a.token_stride : zeros;
-    if ((lane & 31) < TILE) row_at[wave][lane >> 5][tp] = reinterpret_cast<uint64_t>(row);
+    if (TILE == 32 || (lane & 16) == 0) row_at[wave][lane >> 5][tp] = reinterpret_cast<uint64_t>(row);
     const uint32_t kept = (uint32_t)__ballot(page >= 0) & EVERY;
     asm volatile("" ::: "memory");  // (a wavefront's LDS operations execute in order)
     return kept;
   };
 
-  u32x4 kr[SUB][KSTEPS];
+  u32x4 kr[SUB][2][LINES];
   VWord vr[NV][NBLK];
+  // 8 keys' whole 128-byte lines per instruction: lane (m16, g) has piece g + 4 (m16 / 8) of key m16 % 8
   auto load_keys = [&]() {
 #pragma unroll
-    for (int st = 0; st < SUB; ++st) {
-      const char* row = reinterpret_cast<const char*>(row_at[wave][0][st * 16 + m16]) + g * 16;
+    for (int st = 0; st < SUB; ++st)
 #pragma unroll
-      for (int s = 0; s < KSTEPS; ++s) {
-        const char* p = row + s * 64;
-        if (!FULL && s * 64 + g * 16 >= a.D * (int)sizeof(X)) p = zeros;
-        kr[st][s] = *reinterpret_cast<const u32x4*>(p);
+      for (int e = 0; e < 2; ++e) {
+        const char* row = reinterpret_cast<const char*>(row_at[wave][0][st * 16 + e * 8 + (m16 & 7)]) + piece;
+#pragma unroll
+        for (int c = 0; c < LINES; ++c) {
+          const char* p = row + c * 128;
+          if (!FULL && c * 128 + piece >= a.D * (int)sizeof(X)) p = zeros;
+          kr[st][e][c] = read<NT, u32x4>(p);
+        }
       }
-    }
   };
   auto load_values = [&]() {
 #pragma unroll
@@ -187,19 +221,11 @@ __global__ __launch_bounds__(64 * WAVES) void decode_kernel(DecodeArgs a) {
       for (int blk = 0; blk < NBLK; ++blk) {
         const char* p = row + blk * (BD * sizeof(X));
         if (!FULL && (blk * 16 + m16) * EPL >= a.D) p = zeros;
-        vr[u][blk] = *reinterpret_cast<const VWord*>(p);
+        vr[u][blk] = read<NT, VWord>(p);
       }
     }
   };
 
-  int entry = page_of(t), entry_next = page_of(t + WAVES);
-  u32x4 qr[KSTEPS];
-  {
-    const bool have = m16 < my_heads;
-    const char* row = a.q + (int64_t)ch.b * a.q_token + (int64_t)(hk * a.G + ht * HEADS + m16) * a.q_head + g * 16;
-#pragma unroll
-    for (int s = 0; s < KSTEPS; ++s) qr[s] = *reinterpret_cast<const u32x4*>(have && (s * 64 + g * 16) < a.D * (int)sizeof(X) ? row + s * 64 : zeros);
-  }
   const float slope = a.slopes && m16 < my_heads ? a.slopes[hk * a.G + ht * HEADS + m16] : 0.f;
   const bool plain = a.cap == 0.f && !a.slopes;
   const float scale2 = a.scale * LOG2E;
@@ -211,36 +237,45 @@ __global__ __launch_bounds__(64 * WAVES) void decode_kernel(DecodeArgs a) {
 #pragma unroll
     for (int j = 0; j < EPL; ++j) o[blk][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  uint32_t kept = 0;
   if (t < t_end) {
-    kept = place_rows(t, entry);
+    u32x4 qr[KSTEPS];
+    const bool have = m16 < my_heads;
+    const char* q_row = a.q + (int64_t)ch.b * a.q_token + (int64_t)(hk * a.G + ht * HEADS + m16) * a.q_head + g * 16;
+#pragma unroll
+    for (int s = 0; s < KSTEPS; ++s) qr[s] = read<false, u32x4>(have && (s * 64 + g * 16) < a.D * (int)sizeof(X) ? q_row + s * 64 : zeros);
+    const int now = entry_of(t);
+    int entry = entry_of(t + step);
+    uint32_t kept = place_rows(t, now);
+    __builtin_amdgcn_sched_barrier(0);  // (the loop counts on the keys being requested first)
     load_keys();
+    __builtin_amdgcn_sched_barrier(0);
     load_values();
-  }
-  for (; t < t_end; t += WAVES) {
+  do {
     const uint32_t here = kept;
-    entry = entry_next;
-    entry_next = page_of(t + 2 * WAVES);
+    const int entry_next = entry_of(t + 2 * step);
     f32x4 z[SUB];
 #pragma unroll
     for (int st = 0; st < SUB; ++st) {
-      z[st] = f32x4{0.f, 0.f, 0.f, 0.f};
+      // [e][h]: keys e*8.. by the pieces 4h..4h+3 of their lines; rows 8h..8h+7 of the product are the ones that mean something
+      f32x4 part[2][2];
 #pragma unroll
-      for (int s = 0; s < KSTEPS; ++s) {
-        if constexpr (BF16) {
-          z[st] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[st][s]), __builtin_bit_cast(bf16x8, qr[s]), z[st], 0, 0, 0);
-        } else {
+      for (int e = 0; e < 2; ++e)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            z[st] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[st][s][e]), __uint_as_float(qr[s][e]), z[st], 0, 0, 0);
+        for (int h = 0; h < 2; ++h) {
+          part[e][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int c = 0; c < LINES; ++c) part[e][h] = product<BF16>(kr[st][e][c], qr[2 * c + h], part[e][h]);
         }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        // a place's other half lies 32 lanes away
+        const float mine = lane < 32 ? part[0][0][i] : part[1][1][i], other = lane < 32 ? part[1][0][i] : part[0][1][i];
+        z[st][i] = mine + other_half(other, lane);
       }
     }
-    const bool more = t + WAVES < t_end;
-    if (more) {
-      kept = place_rows(t + WAVES, entry);
-      load_keys();
-    }
+    kept = place_rows(t + step, entry);
+    entry = entry_next;
+    load_keys();
     // scores in units of log 2
     if (plain) {
 #pragma unroll
@@ -322,7 +357,9 @@ __global__ __launch_bounds__(64 * WAVES) void decode_kernel(DecodeArgs a) {
           for (int j = 0; j < EPL; ++j)
             o[blk][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[i][blk][j]), z[0][i], o[blk][j], 0, 0, 0);
     }
-    if (more) load_values();
+    load_values();
+    t += step;
+  } while (t < t_end);
   }
 
   // the wavefronts' parts: common maximum, then the sum through LDS
@@ -330,14 +367,14 @@ __global__ __launch_bounds__(64 * WAVES) void decode_kernel(DecodeArgs a) {
   l += __shfl_xor(l, 32, 64);
   if (g == 0) ml_lds[wave][m16] = f32x2{m, l};
   __syncthreads();
-  auto joined_max = [&](int head) {
-    float top = ml_lds[0][head][0];
-#pragma unroll
-    for (int w = 1; w < WAVES; ++w) top = fmaxf(top, ml_lds[w][head][0]);
+  // (wavefront w and those a multiple of wave_heads away have the same kv head)
+  auto joined_max = [&](int w, int row) {
+    float top = -INFINITY;
+    for (w %= a.wave_heads; w < WAVES; w += a.wave_heads) top = fmaxf(top, ml_lds[w][row][0]);
     return top;
   };
-  auto part_weight = [&](int w, int head, float top) { return top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml_lds[w][head][0] - top); };
-  const float f = m16 < my_heads ? part_weight(wave, m16, joined_max(m16)) : 0.f;
+  auto part_weight = [&](int w, int row, float top) { return top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml_lds[w][row][0] - top); };
+  const float f = m16 < my_heads ? part_weight(wave, m16, joined_max(wave, m16)) : 0.f;
   const int d = threadIdx.x % (BD / 4) * 4;
 #pragma unroll
   for (int blk = 0; blk < NBLK; ++blk) {
@@ -353,21 +390,20 @@ __global__ __launch_bounds__(64 * WAVES) void decode_kernel(DecodeArgs a) {
     }
     __syncthreads();
     const int dim = blk * BD + d;
-    for (int r = threadIdx.x / (BD / 4); r < my_heads; r += 64 * WAVES / (BD / 4)) {
-      const float top = joined_max(r);
+    for (int i = threadIdx.x / (BD / 4); i < my_heads * a.wave_heads; i += 64 * WAVES / (BD / 4)) {
+      const int wh = i / my_heads, r = i % my_heads, head = item - wave % a.wave_heads + wh;  // the head's item
+      const float top = joined_max(wh, r);
       float sum = 0.f;
       f32x4 y{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int w = 0; w < WAVES; ++w) {
+      for (int w = wh; w < WAVES; w += a.wave_heads) {
         sum += ml_lds[w][r][1] * part_weight(w, r, top);
         y += *reinterpret_cast<const f32x4*>(o_lds + (w * a.rows + r) * PITCH + d);
       }
       if (!FULL && dim >= a.D) continue;
-      const int h = hk * a.G + ht * HEADS + r;
       if (ch.n == 1) {
-        store_row<X>(a, ch.b, h, dim, y, sum, top);
+        store_row<X>(a, ch.b, head % a.hkv * a.G + ht * HEADS + r, dim, y, sum, top);
       } else {
-        const int64_t at = (int64_t)blockIdx.x * a.rows + r;
+        const int64_t at = ((int64_t)pos * a.items + head) * a.rows + r;
         *reinterpret_cast<f32x4*>(a.part_o + at * a.D + dim) = y;
         if (dim == 0) a.part_ml[at] = f32x2{top, sum};
       }
@@ -379,44 +415,60 @@ __global__ __launch_bounds__(64 * WAVES) void decode_kernel(DecodeArgs a) {
 constexpr int JOIN_THREADS = 256;
 template <typename X>
 __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(DecodeArgs a) {
+  constexpr int AHEAD = 8, JW = JOIN_THREADS / 64;
   extern __shared__ __attribute__((aligned(16))) float weight[];  // one per chunk
-  __shared__ float red[JOIN_THREADS / 64];
+  __shared__ float red[2][JW];
   __shared__ f32x4 sums[JOIN_THREADS];
   const int b = blockIdx.x / a.hq, h = blockIdx.x % a.hq;
   const int2 plan = a.plan[b];
   if (plan.y <= 1) return;
   const int hk = h / a.G, r = h % a.G % HEADS, item = h % a.G / HEADS * a.hkv + hk;
-  auto at = [&](int j) { return ((int64_t)(plan.x + j) * a.items + item) * a.rows + r; };
+  const int64_t row0 = ((int64_t)plan.x * a.items + item) * a.rows + r, row_step = (int64_t)a.items * a.rows;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int across = a.D <= 64 ? 16 : a.D <= 128 ? 32 : 64, d = tid % across * 4, groups = JOIN_THREADS / across, first = tid / across;
+  f32x4 part[AHEAD];
+  // the first rows are requested before their weights are known
+  auto request = [&](int j0) {
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int j = j0 + u * groups;
+      part[u] = j < plan.y && d < a.D ? *reinterpret_cast<const f32x4*>(a.part_o + (row0 + j * row_step) * a.D + d) : f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  };
   float top = -INFINITY;
-  for (int j = tid; j < plan.y; j += JOIN_THREADS) top = fmaxf(top, a.part_ml[at(j)][0]);
+  for (int j = tid; j < plan.y; j += JOIN_THREADS) top = fmaxf(top, a.part_ml[row0 + j * row_step][0]);
+  request(first);
 #pragma unroll
   for (int s = 32; s; s >>= 1) top = fmaxf(top, __shfl_xor(top, s, 64));
-  if (lane == 0) red[wave] = top;
-  __syncthreads();
+  if (lane == 0) red[0][wave] = top;
+  lds_barrier();
 #pragma unroll
-  for (int w = 0; w < JOIN_THREADS / 64; ++w) top = fmaxf(top, red[w]);
-  __syncthreads();
+  for (int w = 0; w < JW; ++w) top = fmaxf(top, red[0][w]);
   float sum = 0.f;
   for (int j = tid; j < plan.y; j += JOIN_THREADS) {
-    const f32x2 ml = a.part_ml[at(j)];
+    const f32x2 ml = a.part_ml[row0 + j * row_step];
     const float f = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[0] - top);
     weight[j] = f;
     sum += f * ml[1];
   }
 #pragma unroll
   for (int s = 32; s; s >>= 1) sum += __shfl_xor(sum, s, 64);
-  if (lane == 0) red[wave] = sum;
-  __syncthreads();
+  if (lane == 0) red[1][wave] = sum;
+  lds_barrier();
   sum = 0.f;
 #pragma unroll
-  for (int w = 0; w < JOIN_THREADS / 64; ++w) sum += red[w];
-  const int across = a.D <= 64 ? 16 : a.D <= 128 ? 32 : 64, d = tid % across * 4, groups = JOIN_THREADS / across;
+  for (int w = 0; w < JW; ++w) sum += red[1][w];
   f32x4 y{0.f, 0.f, 0.f, 0.f};
-  if (d < a.D)
-    for (int j = tid / across; j < plan.y; j += groups) y += weight[j] * *reinterpret_cast<const f32x4*>(a.part_o + at(j) * a.D + d);
+  for (int j0 = first;;) {
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (j0 + u * groups < plan.y) y += weight[j0 + u * groups] * part[u];
+    j0 += AHEAD * groups;
+    if (j0 >= plan.y) break;
+    request(j0);
+  }
   sums[tid] = y;
-  __syncthreads();
+  lds_barrier();
   if (tid >= across || d >= a.D) return;
   for (int i = 1; i < groups; ++i) y += sums[tid + i * across];
   store_row<X>(a, b, h, d, y, sum, top);
@@ -424,7 +476,8 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(DecodeArgs a) {
 
 // The split of a call: what its grid, its workspace and its kernels agree on.
 struct Split {
-  int rows, items, least;
+  int rows, items, wave_heads, least;
+  bool nt;
   int64_t chunks, tiles;  // most chunks of a batch, most tiles of a sequence
   size_t ml, o, total;    // bytes: offsets of the parts (the plan lies in front)
 };
@@ -434,9 +487,12 @@ Split split_of(const moe_kv_cache* c, int32_t n_q_heads) {
   const int G = n_q_heads / c->n_kv_heads, tile = c->dtype == MOE_BF16 ? 32 : 16;
   s.rows = G < HEADS ? G : HEADS;
   s.items = c->n_kv_heads * ((G + HEADS - 1) / HEADS);
-  s.least = LEAST_PLACES / tile;
+  // Pools whose heads are neighbours in memory are read a group of heads at a time.
+  s.wave_heads = c->head_stride < c->token_stride ? (c->n_kv_heads % 4 == 0 ? 4 : c->n_kv_heads % 2 == 0 ? 2 : 1) : 1;
+  s.least = 2 * WAVES / s.wave_heads;
   s.tiles = ((int64_t)c->table_width * c->page_size + tile - 1) / tile;
-  s.chunks = most_chunks(c->n_seqs, s.items, TARGET_WORKGROUPS, s.least, s.tiles);
+  s.chunks = most_chunks(c->n_seqs, s.items / s.wave_heads, TARGET_WORKGROUPS, s.least, s.tiles);
+  s.nt = (double)c->n_pages * c->page_size * c->n_kv_heads * c->head_dim * 2 * elem_size(c->dtype) > (double)(300 << 20);
   s.ml = align_up((size_t)c->n_seqs * sizeof(int2), 256);
   s.o = s.ml + align_up((size_t)s.chunks * s.items * s.rows * sizeof(f32x2), 256);
   s.total = s.o + align_up((size_t)s.chunks * s.items * s.rows * c->head_dim * sizeof(float), 256);
@@ -444,22 +500,28 @@ Split split_of(const moe_kv_cache* c, int32_t n_q_heads) {
   return s;
 }
 
-template <typename X, int DP>
+template <typename X, int DP, bool NT>
 void launch(const DecodeArgs& a, unsigned grid, hipStream_t s) {
   const size_t lds = (size_t)WAVES * a.rows * (16 * Shape<X, DP>::EPL + 4) * sizeof(float);
-  if (a.D == DP) hipLaunchKernelGGL((decode_kernel<X, DP, true>), dim3(grid), dim3(64 * WAVES), lds, s, a);
-  else hipLaunchKernelGGL((decode_kernel<X, DP, false>), dim3(grid), dim3(64 * WAVES), lds, s, a);
+  if (a.D == DP) hipLaunchKernelGGL((decode_kernel<X, DP, true, NT>), dim3(grid), dim3(64 * WAVES), lds, s, a);
+  else hipLaunchKernelGGL((decode_kernel<X, DP, false, NT>), dim3(grid), dim3(64 * WAVES), lds, s, a);
+}
+
+template <typename X, int DP>
+void launch(const DecodeArgs& a, unsigned grid, bool nt, hipStream_t s) {
+  if (nt) launch<X, DP, true>(a, grid, s);
+  else launch<X, DP, false>(a, grid, s);
 }
 
 template <typename X>
 int32_t launch_decode(const DecodeArgs& a, const Split& sp, hipStream_t s) {
-  const unsigned grid = (unsigned)(sp.chunks * sp.items);
-  if (a.D <= 64) launch<X, 64>(a, grid, s);
-  else if (a.D <= 128) launch<X, 128>(a, grid, s);
-  else launch<X, 256>(a, grid, s);
+  const unsigned grid = (unsigned)(sp.chunks * sp.items / a.wave_heads);
+  if (a.D <= 64) launch<X, 64>(a, grid, sp.nt, s);
+  else if (a.D <= 128) launch<X, 128>(a, grid, sp.nt, s);
+  else launch<X, 256>(a, grid, sp.nt, s);
   int32_t st = check_hip(hipGetLastError(), "attention launch");
   if (st != MOE_OK || sp.tiles <= sp.least) return st;  // (no sequence can have two chunks)
-  const size_t weights = (size_t)(TARGET_WORKGROUPS / sp.items + 2) * sizeof(float);
+  const size_t weights = (size_t)(TARGET_WORKGROUPS * a.wave_heads / sp.items + 2) * sizeof(float);
   hipLaunchKernelGGL(join_kernel<X>, dim3((unsigned)(a.n_seqs * a.hq)), dim3(JOIN_THREADS), weights, s, a);
   return check_hip(hipGetLastError(), "attention join launch");
 }
@@ -528,6 +590,7 @@ extern "C" int32_t moe_attention_decode(const moe_kv_cache* c, int32_t n_q_heads
   a.G = n_q_heads / c->n_kv_heads;
   a.rows = sp.rows;
   a.items = sp.items;
+  a.wave_heads = sp.wave_heads;
   a.D = c->head_dim;
   a.window = opt->window;
   a.least = sp.least;
