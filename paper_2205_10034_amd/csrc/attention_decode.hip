@@ -29,12 +29,17 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int WAVES = 4;
 constexpr int HEADS = 16;  // query heads of a tile
-constexpr int TARGET_WORKGROUPS = 1024;
+constexpr int LEAST_PER_WAVE = 2, MANY_ROWS = 1024;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 // Rows of places that are not there and dimensions beyond head_dim are read from here: no load leaves the caller's rows, and what
 // lies in places that are not kept reaches no product.
 __device__ const u32x4 ZEROS[MOE_MAX_HEAD_DIM * 4 / 16] = {};
+
+// Workgroups of the decode kernel that a CU holds: two need up to 256 registers a lane, which keys and values of 128 dimensions on
+// their way leave room for; a third or a fourth costs registers for what is in flight (64 sequences, 1.3 GB: 210 us with two,
+// 237 with three), and 256 dimensions need more than 256 (130 MB: 48 us with one, 64 with two, which spill).
+constexpr int resident_workgroups(int dims) { return dims <= 128 ? 2 : 1; }
 
 struct DecodeArgs {
   const char *k, *v, *q;
@@ -42,13 +47,14 @@ struct DecodeArgs {
   float* lse;
   const int32_t *table, *lens;
   const float* slopes;
-  float* part_o;   // [chunk*items][rows][D]
-  f32x2* part_ml;  // [chunk*items][rows]
-  int2* plan;      // [sequence]: first chunk, chunks
+  float* part_o;   // [slot][items][rows][D]
+  f32x2* part_ml;  // [slot][items][rows]
+  int2* plan;      // [sequence]: slot of the first piece, pieces
   int64_t n_pages, page_stride, token_stride, head_stride, q_token, q_head, o_token, o_head;  // bytes
   PageDivisor page;
-  int32_t page_size, table_width, n_seqs, hq, hkv, G, rows, items, wave_heads, D, window, least;
+  int32_t page_size, table_width, n_seqs, hq, hkv, G, rows, items, hts, wave_heads, parts, D, window, least;
   float scale, cap, inv_cap;
+  double inverse_parts;
 };
 
 template <typename X, int DP> struct Shape;
@@ -63,44 +69,49 @@ template <int BYTES> struct Words;
 template <> struct Words<8> { typedef u32x2 type; };
 template <> struct Words<16> { typedef u32x4 type; };
 
-struct Chunk {
-  int b, j, n, first;  // sequence, which of its n chunks; the sequence's first chunk
-};
-
-__device__ __forceinline__ int tiles_of(const DecodeArgs& a, int b, int tile) {
-  const int n = kept_length(a.lens[b], a.table_width * a.page_size);
-  return kept_tiles(n, first_place(n, a.window), tile);
+// A value that all lanes hold, for the scalar registers.
+__device__ __forceinline__ int64_t uniform(int64_t v, int lane) {
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)v, lane), hi = __builtin_amdgcn_readlane((int)(v >> 32), lane);
+  return (int64_t)(((uint64_t)hi << 32) | lo);
 }
 
-// Chunk number `pos` of the batch; every wavefront finds it by itself.  False: there are fewer chunks.
-__device__ __forceinline__ bool find_chunk(const DecodeArgs& a, int tile, int groups, int pos, Chunk* out) {
+// Where part `w` of the row of tiles begins; every wavefront finds it by itself.
+struct Position {
+  int64_t share, total;  // tiles of a part, of the row
+  int64_t begin;         // the sequence's first tile in the row
+  int b, n;              // sequence, its kept length
+};
+__device__ __forceinline__ int length_of(const DecodeArgs& a, int b) { return kept_length(a.lens[b], a.table_width * a.page_size); }
+__device__ __forceinline__ Position find_part(const DecodeArgs& a, int tile, int w) {
   const int lane = threadIdx.x & 63;
-  int64_t total = 0;
-  for (int s = lane; s < a.n_seqs; s += 64) total += tiles_of(a, s, tile);
-#pragma unroll
-  for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d, 64);
-  const int c = chunk_tiles(total, groups, TARGET_WORKGROUPS, a.least);
-  int before = 0;
-  for (int s = 0; s < a.n_seqs; s += 64) {
-    const int n = s + lane < a.n_seqs ? chunk_count(tiles_of(a, s + lane, tile), c) : 0;
-    int upto = n;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int other = __shfl_up(upto, d, 64);
+  auto in_row = [&](int n) { return row_tiles(kept_tiles(n, first_place(n, a.window), tile)); };
+  int n = lane < a.n_seqs ? length_of(a, lane) : 0;
+  int64_t mine = lane < a.n_seqs ? in_row(n) : 0, total = mine;
+  for (int s = lane + 64; s < a.n_seqs; s += 64) total += in_row(length_of(a, s));
+  for (int d = 1; d < 64 && d < a.n_seqs; d <<= 1) total += __shfl_xor(total, d, 64);
+  total = uniform(total, 0);
+  Position p{uniform(share_of_row(total, a.inverse_parts, a.least), 0), total, 0, 0, 0};
+  const int64_t at = w * p.share;
+  if (at >= total) return p;
+  for (int s = 0;;) {
+    int64_t upto = mine;
+    for (int d = 1; d < 64 && d < a.n_seqs; d <<= 1) {
+      const int64_t other = __shfl_up(upto, d, 64);
       if (lane >= d) upto += other;
     }
-    const unsigned long long beyond = __ballot(before + upto > pos);
+    const unsigned long long beyond = __ballot(p.begin + upto > at);
     if (beyond) {
       const int who = __ffsll(beyond) - 1;
-      out->b = s + who;
-      out->n = __builtin_amdgcn_readlane(n, who);
-      out->first = before + __builtin_amdgcn_readlane(upto, who) - out->n;
-      out->j = pos - out->first;
-      return true;
+      p.b = s + who;
+      p.n = __builtin_amdgcn_readlane(n, who);
+      p.begin += uniform(upto - mine, who);
+      return p;
     }
-    before += __builtin_amdgcn_readlane(upto, 63);
+    p.begin += uniform(upto, 63);
+    s += 64;
+    n = s + lane < a.n_seqs ? length_of(a, s + lane) : 0;
+    mine = s + lane < a.n_seqs ? in_row(n) : 0;
   }
-  return false;
 }
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -148,7 +159,7 @@ __device__ __forceinline__ void store_row(const DecodeArgs& a, int b, int h, int
 // One (sequence, kv head, tile of query heads, chunk of places) per workgroup; its wavefronts take the chunk's tiles in turn.
 // FULL: head_dim is DP, no lane's dimensions lie beyond it.
 template <typename X, int DP, bool FULL, bool NT>
-__global__ __launch_bounds__(64 * WAVES) void decode_kernel(DecodeArgs a) {
+__global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP)) void decode_kernel(DecodeArgs a) {
   using S = Shape<X, DP>;
   constexpr bool BF16 = sizeof(X) == 2;
   constexpr int SUB = S::SUB, TILE = 16 * SUB, EPL = S::EPL, KSTEPS = S::KSTEPS, LINES = KSTEPS / 2, NV = 4 * SUB, BD = 16 * EPL, NBLK = DP / BD, PITCH = BD + 4;
@@ -161,35 +172,47 @@ __global__ __launch_bounds__(64 * WAVES) void decode_kernel(DecodeArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m16 = lane & 15, g = lane >> 4, piece = (g + 4 * (m16 >> 3)) * 16;
   // wavefronts of a workgroup: wave_heads neighbouring kv heads, `step` of them on the tiles of each in turn
-  const int groups = a.items / a.wave_heads, pos = blockIdx.x / groups, step = WAVES / a.wave_heads;
-  const int item = blockIdx.x % groups * a.wave_heads + wave % a.wave_heads, hk = item % a.hkv, ht = item / a.hkv;
-  Chunk ch;
-  if (!find_chunk(a, TILE, groups, pos, &ch)) return;
-  const int n = kept_length(a.lens[ch.b], a.table_width * a.page_size), first = first_place(n, a.window);
-  const int tile0 = first / TILE, tiles = kept_tiles(n, first, TILE);
-  const int t_end = tile0 + chunk_begin(tiles, ch.n, ch.j + 1);
-  int t = tile0 + chunk_begin(tiles, ch.n, ch.j) + wave / a.wave_heads;
-  const int my_heads = a.G - ht * HEADS < HEADS ? a.G - ht * HEADS : HEADS;
-  if (threadIdx.x == 0 && item == 0 && ch.j == 0) a.plan[ch.b] = make_int2(ch.first, ch.n);
-
+  const int groups = a.items / a.wave_heads, w = blockIdx.x / groups, step = WAVES / a.wave_heads;
+  const int item = blockIdx.x % groups * a.wave_heads + wave % a.wave_heads, hk = item / a.hts, ht = item % a.hts;
+  auto heads_of = [&](int tile_of_heads) { return a.G - tile_of_heads * HEADS < HEADS ? a.G - tile_of_heads * HEADS : HEADS; };
+  const int my_heads = heads_of(ht);
   const char* zeros = reinterpret_cast<const char*>(ZEROS);
   const char* base = (lane < 32 ? a.k : a.v) + hk * a.head_stride;  // lanes 0-31 place the keys' rows, the others the values'
-  const int32_t* table = a.table + (int64_t)ch.b * a.table_width;
   const int tp = lane & (TILE - 1);
+  const bool plain = a.cap == 0.f && !a.slopes;
+  const float scale2 = a.scale * LOG2E;
+  const float slope = a.slopes && m16 < my_heads ? a.slopes[hk * a.G + ht * HEADS + m16] : 0.f;
+
+  Position at = find_part(a, TILE, w);
+  int64_t x = w * at.share;
+  const int64_t x_end = x + at.share < at.total ? x + at.share : at.total;
+  for (int piece_no = 0; x < x_end; ++piece_no) {
+  // the piece of sequence b that lies in this part
+  const int b = at.b;
+  const int n = at.n, first = first_place(n, a.window), tile0 = first / TILE, tiles = kept_tiles(n, first, TILE);
+  const int64_t b_end = at.begin + row_tiles(tiles);
+  const int from = (int)(x - at.begin), upto = b_end < x_end ? tiles : (int)(x_end - at.begin);
+  const bool whole = from == 0 && b_end <= x_end;
+  const int slot = 2 * w + (piece_no > 0);
+  if (from == 0 && threadIdx.x == 0 && item == 0)
+    a.plan[b] = make_int2(slot, whole ? 1 : (int)((b_end - 1) / at.share) - w + 1);
+  const int t_end = tiles ? tile0 + upto : 0;
+  int t = tile0 + from + wave / a.wave_heads;
+  const int32_t* table = a.table + (int64_t)b * a.table_width;
 
   // Nothing in the loop that loads is conditional: what a tile beyond the last one would load is ZEROS.  (Behind a branch the
   // compiler waits for every load in flight before it uses the first.)
   auto is_kept = [&](int tt) {
-    const int p = tt * TILE + tp;
+    const int p = (int)((unsigned)tt * TILE + tp);
     return tt < t_end && p >= first && p < n;
   };
   // the table's entry for this lane's place of tile tt
-  auto entry_of = [&](int tt) { return table[is_kept(tt) ? a.page.quotient(tt * TILE + tp) : 0]; };
+  auto entry_of = [&](int tt) { return table[is_kept(tt) ? a.page.quotient((int)((unsigned)tt * TILE + tp)) : 0]; };
   // rows of tile tt into LDS; returns which places are kept
   auto place_rows = [&](int tt, int entry) {
-    const int p = tt * TILE + tp, page = is_kept(tt) ? valid_page(entry, a.n_pages) : -1;
-    const int slot = p - a.page.quotient(p) * a.page_size;
-    const char* row = page >= 0 ? base + page * a.page_stride + slot * a.token_stride : zeros;
+    const int p = (int)((unsigned)tt * TILE + tp), page = is_kept(tt) ? valid_page(entry, a.n_pages) : -1;
+    const int in_page = p - a.page.quotient(p) * a.page_size;
+    const char* row = page >= 0 ? base + page * a.page_stride + in_page * a.token_stride : zeros;
     if (TILE == 32 || (lane & 16) == 0) row_at[wave][lane >> 5][tp] = reinterpret_cast<uint64_t>(row);
     const uint32_t kept = (uint32_t)__ballot(page >= 0) & EVERY;
     asm volatile("" ::: "memory");  // (a wavefront's LDS operations execute in order)
@@ -226,10 +249,6 @@ __global__ __launch_bounds__(64 * WAVES) void decode_kernel(DecodeArgs a) {
     }
   };
 
-  const float slope = a.slopes && m16 < my_heads ? a.slopes[hk * a.G + ht * HEADS + m16] : 0.f;
-  const bool plain = a.cap == 0.f && !a.slopes;
-  const float scale2 = a.scale * LOG2E;
-
   float m = -INFINITY, mref = 0.f, l = 0.f;
   f32x4 o[NBLK][EPL];
 #pragma unroll
@@ -240,7 +259,7 @@ __global__ __launch_bounds__(64 * WAVES) void decode_kernel(DecodeArgs a) {
   if (t < t_end) {
     u32x4 qr[KSTEPS];
     const bool have = m16 < my_heads;
-    const char* q_row = a.q + (int64_t)ch.b * a.q_token + (int64_t)(hk * a.G + ht * HEADS + m16) * a.q_head + g * 16;
+    const char* q_row = a.q + (int64_t)b * a.q_token + (int64_t)(hk * a.G + ht * HEADS + m16) * a.q_head + g * 16;
 #pragma unroll
     for (int s = 0; s < KSTEPS; ++s) qr[s] = read<false, u32x4>(have && (s * 64 + g * 16) < a.D * (int)sizeof(X) ? q_row + s * 64 : zeros);
     const int now = entry_of(t);
@@ -365,8 +384,9 @@ __global__ __launch_bounds__(64 * WAVES) void decode_kernel(DecodeArgs a) {
   // the wavefronts' parts: common maximum, then the sum through LDS
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
+  lds_barrier();  // (the piece before has been read)
   if (g == 0) ml_lds[wave][m16] = f32x2{m, l};
-  __syncthreads();
+  lds_barrier();
   // (wavefront w and those a multiple of wave_heads away have the same kv head)
   auto joined_max = [&](int w, int row) {
     float top = -INFINITY;
@@ -378,7 +398,7 @@ __global__ __launch_bounds__(64 * WAVES) void decode_kernel(DecodeArgs a) {
   const int d = threadIdx.x % (BD / 4) * 4;
 #pragma unroll
   for (int blk = 0; blk < NBLK; ++blk) {
-    if (blk) __syncthreads();
+    if (blk) lds_barrier();
     if (m16 < my_heads) {
       float* row = o_lds + (wave * a.rows + m16) * PITCH;
 #pragma unroll
@@ -388,10 +408,11 @@ __global__ __launch_bounds__(64 * WAVES) void decode_kernel(DecodeArgs a) {
           *reinterpret_cast<f32x4*>(row + (g * 4 + i) * EPL + j) =
               f32x4{o[blk][j][i] * f, o[blk][j + 1][i] * f, o[blk][j + 2][i] * f, o[blk][j + 3][i] * f};
     }
-    __syncthreads();
+    lds_barrier();
     const int dim = blk * BD + d;
-    for (int i = threadIdx.x / (BD / 4); i < my_heads * a.wave_heads; i += 64 * WAVES / (BD / 4)) {
-      const int wh = i / my_heads, r = i % my_heads, head = item - wave % a.wave_heads + wh;  // the head's item
+    for (int i = threadIdx.x / (BD / 4); i < a.rows * a.wave_heads; i += 64 * WAVES / (BD / 4)) {
+      const int wh = i / a.rows, r = i % a.rows, its = item - wave % a.wave_heads + wh;  // the row's item
+      if (r >= heads_of(its % a.hts)) continue;
       const float top = joined_max(wh, r);
       float sum = 0.f;
       f32x4 y{0.f, 0.f, 0.f, 0.f};
@@ -400,64 +421,77 @@ __global__ __launch_bounds__(64 * WAVES) void decode_kernel(DecodeArgs a) {
         y += *reinterpret_cast<const f32x4*>(o_lds + (w * a.rows + r) * PITCH + d);
       }
       if (!FULL && dim >= a.D) continue;
-      if (ch.n == 1) {
-        store_row<X>(a, ch.b, head % a.hkv * a.G + ht * HEADS + r, dim, y, sum, top);
+      if (whole) {
+        store_row<X>(a, b, its / a.hts * a.G + its % a.hts * HEADS + r, dim, y, sum, top);
       } else {
-        const int64_t at = ((int64_t)pos * a.items + head) * a.rows + r;
-        *reinterpret_cast<f32x4*>(a.part_o + at * a.D + dim) = y;
-        if (dim == 0) a.part_ml[at] = f32x2{top, sum};
+        const int64_t part = ((int64_t)slot * a.items + its) * a.rows + r;
+        *reinterpret_cast<f32x4*>(a.part_o + part * a.D + dim) = y;
+        if (dim == 0) a.part_ml[part] = f32x2{top, sum};
       }
     }
   }
+  x = b_end;
+  at.begin = b_end;
+  if (x < x_end) at.n = length_of(a, ++at.b);
+  }
 }
 
-// Joins the chunks of one (sequence, query head) in their order; sequences of one chunk are complete already.
+// Joins the pieces of (sequence, query head) rows in their order; sequences of one piece are complete already.  ROW threads work on a
+// row: a wavefront where there are many rows, of few pieces each, a whole workgroup where there are few.
 constexpr int JOIN_THREADS = 256;
-template <typename X>
+template <typename X, int ROW>
 __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(DecodeArgs a) {
-  constexpr int AHEAD = 8, JW = JOIN_THREADS / 64;
-  extern __shared__ __attribute__((aligned(16))) float weight[];  // one per chunk
-  __shared__ float red[2][JW];
+  constexpr int AHEAD = 8, WIDE = ROW / 64;
+  extern __shared__ __attribute__((aligned(16))) float weights[];  // one per piece and row
+  __shared__ float red[2][WIDE];
   __shared__ f32x4 sums[JOIN_THREADS];
-  const int b = blockIdx.x / a.hq, h = blockIdx.x % a.hq;
+  auto barrier = [] {
+    if (WIDE > 1) lds_barrier();
+    else asm volatile("" ::: "memory");  // (a wavefront's LDS operations execute in order)
+  };
+  const int id = blockIdx.x * (JOIN_THREADS / ROW) + threadIdx.x / ROW;
+  if (id >= a.n_seqs * a.hq) return;
+  const int b = id / a.hq, h = id % a.hq;
   const int2 plan = a.plan[b];
   if (plan.y <= 1) return;
-  const int hk = h / a.G, r = h % a.G % HEADS, item = h % a.G / HEADS * a.hkv + hk;
-  const int64_t row0 = ((int64_t)plan.x * a.items + item) * a.rows + r, row_step = (int64_t)a.items * a.rows;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int across = a.D <= 64 ? 16 : a.D <= 128 ? 32 : 64, d = tid % across * 4, groups = JOIN_THREADS / across, first = tid / across;
+  const int hk = h / a.G, r = h % a.G % HEADS, item = hk * a.hts + h % a.G / HEADS;
+  auto row = [&](int j) { return ((int64_t)piece_slot(plan.x, j) * a.items + item) * a.rows + r; };
+  const int tid = threadIdx.x % ROW, lane = tid & 63, wave = tid >> 6;
+  float* weight = weights + threadIdx.x / ROW * a.parts;
+  const int across = a.D <= 64 ? 16 : a.D <= 128 ? 32 : 64, d = tid % across * 4, groups = ROW / across, first = tid / across;
   f32x4 part[AHEAD];
   // the first rows are requested before their weights are known
   auto request = [&](int j0) {
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
       const int j = j0 + u * groups;
-      part[u] = j < plan.y && d < a.D ? *reinterpret_cast<const f32x4*>(a.part_o + (row0 + j * row_step) * a.D + d) : f32x4{0.f, 0.f, 0.f, 0.f};
+      part[u] = j < plan.y && d < a.D ? *reinterpret_cast<const f32x4*>(a.part_o + row(j) * a.D + d) : f32x4{0.f, 0.f, 0.f, 0.f};
     }
   };
+  auto over_row = [&](float v, int which, auto join) {
+#pragma unroll
+    for (int s = 32; s; s >>= 1) v = join(v, __shfl_xor(v, s, 64));
+    if (WIDE == 1) return v;
+    if (lane == 0) red[which][wave] = v;
+    lds_barrier();
+    v = red[which][0];
+#pragma unroll
+    for (int w = 1; w < WIDE; ++w) v = join(v, red[which][w]);
+    return v;
+  };
   float top = -INFINITY;
-  for (int j = tid; j < plan.y; j += JOIN_THREADS) top = fmaxf(top, a.part_ml[row0 + j * row_step][0]);
+  for (int j = tid; j < plan.y; j += ROW) top = fmaxf(top, a.part_ml[row(j)][0]);
   request(first);
-#pragma unroll
-  for (int s = 32; s; s >>= 1) top = fmaxf(top, __shfl_xor(top, s, 64));
-  if (lane == 0) red[0][wave] = top;
-  lds_barrier();
-#pragma unroll
-  for (int w = 0; w < JW; ++w) top = fmaxf(top, red[0][w]);
+  top = over_row(top, 0, [](float x, float y) { return fmaxf(x, y); });
   float sum = 0.f;
-  for (int j = tid; j < plan.y; j += JOIN_THREADS) {
-    const f32x2 ml = a.part_ml[row0 + j * row_step];
+  for (int j = tid; j < plan.y; j += ROW) {
+    const f32x2 ml = a.part_ml[row(j)];
     const float f = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[0] - top);
     weight[j] = f;
     sum += f * ml[1];
   }
-#pragma unroll
-  for (int s = 32; s; s >>= 1) sum += __shfl_xor(sum, s, 64);
-  if (lane == 0) red[1][wave] = sum;
-  lds_barrier();
-  sum = 0.f;
-#pragma unroll
-  for (int w = 0; w < JW; ++w) sum += red[1][w];
+  sum = over_row(sum, 1, [](float x, float y) { return x + y; });
+  barrier();
   f32x4 y{0.f, 0.f, 0.f, 0.f};
   for (int j0 = first;;) {
 #pragma unroll
@@ -467,19 +501,19 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(DecodeArgs a) {
     if (j0 >= plan.y) break;
     request(j0);
   }
-  sums[tid] = y;
-  lds_barrier();
+  f32x4* mine = sums + threadIdx.x / ROW * ROW;
+  mine[tid] = y;
+  barrier();
   if (tid >= across || d >= a.D) return;
-  for (int i = 1; i < groups; ++i) y += sums[tid + i * across];
+  for (int i = 1; i < groups; ++i) y += mine[tid + i * across];
   store_row<X>(a, b, h, d, y, sum, top);
 }
 
 // The split of a call: what its grid, its workspace and its kernels agree on.
 struct Split {
-  int rows, items, wave_heads, least;
+  int rows, items, wave_heads, least, parts;
   bool nt;
-  int64_t chunks, tiles;  // most chunks of a batch, most tiles of a sequence
-  size_t ml, o, total;    // bytes: offsets of the parts (the plan lies in front)
+  size_t ml, o, total;  // bytes: offsets of the pieces (the plan lies in front)
 };
 
 Split split_of(const moe_kv_cache* c, int32_t n_q_heads) {
@@ -487,16 +521,21 @@ Split split_of(const moe_kv_cache* c, int32_t n_q_heads) {
   const int G = n_q_heads / c->n_kv_heads, tile = c->dtype == MOE_BF16 ? 32 : 16;
   s.rows = G < HEADS ? G : HEADS;
   s.items = c->n_kv_heads * ((G + HEADS - 1) / HEADS);
-  // Pools whose heads are neighbours in memory are read a group of heads at a time.
-  s.wave_heads = c->head_stride < c->token_stride ? (c->n_kv_heads % 4 == 0 ? 4 : c->n_kv_heads % 2 == 0 ? 2 : 1) : 1;
-  s.least = 2 * WAVES / s.wave_heads;
-  s.tiles = ((int64_t)c->table_width * c->page_size + tile - 1) / tile;
-  s.chunks = most_chunks(c->n_seqs, s.items / s.wave_heads, TARGET_WORKGROUPS, s.least, s.tiles);
+  // Neighbouring items by one workgroup: tiles of query heads that read the same keys and values, and kv heads whose rows are
+  // neighbours in memory.
+  const bool several = s.items > c->n_kv_heads, neighbours = c->head_stride < c->token_stride;
+  const int wanted = several ? 4 : !neighbours ? 1 : c->head_dim * (int)elem_size(c->dtype) <= 128 ? 4 : 2;
+  s.wave_heads = s.items % wanted == 0 ? wanted : s.items % 2 == 0 && wanted > 1 ? 2 : 1;
+  s.least = LEAST_PER_WAVE * WAVES / s.wave_heads;
+  const int64_t tiles = ((int64_t)c->table_width * c->page_size + tile - 1) / tile, groups = s.items / s.wave_heads;
+  const int64_t resident = 256 * resident_workgroups(c->head_dim) / groups;
+  const int64_t most = (c->n_seqs * (tiles > 0 ? tiles : 1) + s.least - 1) / s.least;
+  s.parts = (int)(most < resident ? most : resident);
+  if (s.parts < 1) s.parts = 1;
   s.nt = (double)c->n_pages * c->page_size * c->n_kv_heads * c->head_dim * 2 * elem_size(c->dtype) > (double)(300 << 20);
   s.ml = align_up((size_t)c->n_seqs * sizeof(int2), 256);
-  s.o = s.ml + align_up((size_t)s.chunks * s.items * s.rows * sizeof(f32x2), 256);
-  s.total = s.o + align_up((size_t)s.chunks * s.items * s.rows * c->head_dim * sizeof(float), 256);
-  if (s.total < 256) s.total = 256;
+  s.o = s.ml + align_up((size_t)s.parts * 2 * s.items * s.rows * sizeof(f32x2), 256);
+  s.total = s.o + align_up((size_t)s.parts * 2 * s.items * s.rows * c->head_dim * sizeof(float), 256);
   return s;
 }
 
@@ -515,14 +554,20 @@ void launch(const DecodeArgs& a, unsigned grid, bool nt, hipStream_t s) {
 
 template <typename X>
 int32_t launch_decode(const DecodeArgs& a, const Split& sp, hipStream_t s) {
-  const unsigned grid = (unsigned)(sp.chunks * sp.items / a.wave_heads);
+  const unsigned grid = (unsigned)(sp.parts * (sp.items / sp.wave_heads));
   if (a.D <= 64) launch<X, 64>(a, grid, sp.nt, s);
   else if (a.D <= 128) launch<X, 128>(a, grid, sp.nt, s);
   else launch<X, 256>(a, grid, sp.nt, s);
   int32_t st = check_hip(hipGetLastError(), "attention launch");
-  if (st != MOE_OK || sp.tiles <= sp.least) return st;  // (no sequence can have two chunks)
-  const size_t weights = (size_t)(TARGET_WORKGROUPS * a.wave_heads / sp.items + 2) * sizeof(float);
-  hipLaunchKernelGGL(join_kernel<X>, dim3((unsigned)(a.n_seqs * a.hq)), dim3(JOIN_THREADS), weights, s, a);
+  if (st != MOE_OK || sp.parts == 1) return st;  // (every sequence was finished)
+  const int64_t rows = (int64_t)a.n_seqs * a.hq;
+  // (a row has about parts / sequences pieces; the weights of four rows' take LDS)
+  if (rows >= MANY_ROWS) {
+    const size_t lds = (size_t)sp.parts * (JOIN_THREADS / 64) * sizeof(float);
+    hipLaunchKernelGGL((join_kernel<X, 64>), dim3((unsigned)((rows * 64 + JOIN_THREADS - 1) / JOIN_THREADS)), dim3(JOIN_THREADS), lds, s, a);
+  } else {
+    hipLaunchKernelGGL((join_kernel<X, JOIN_THREADS>), dim3((unsigned)rows), dim3(JOIN_THREADS), (size_t)sp.parts * sizeof(float), s, a);
+  }
   return check_hip(hipGetLastError(), "attention join launch");
 }
 
@@ -557,7 +602,7 @@ extern "C" int32_t moe_attention_decode(const moe_kv_cache* c, int32_t n_q_heads
   if (!rows_aligned(q, es) || !rows_aligned(out, es))
     return fail(MOE_ERR_INVALID_ARG, "moe_attention_decode: pointers and strides of q and out must be multiples of 16 bytes");
   const Split sp = split_of(c, n_q_heads);
-  if (sp.chunks * sp.items > INT32_MAX || (int64_t)c->n_seqs * n_q_heads > INT32_MAX)
+  if ((int64_t)c->n_seqs * n_q_heads > INT32_MAX)
     return fail(MOE_ERR_UNSUPPORTED, "moe_attention_decode: %d sequences of %d query heads are too many for one call", c->n_seqs, n_q_heads);
   if (!ws || ((uintptr_t)ws & 255) || ws_bytes < need)
     return fail(MOE_ERR_WORKSPACE, "moe_attention_decode: workspace NULL, misaligned or smaller than %zu bytes", need);
@@ -591,9 +636,12 @@ extern "C" int32_t moe_attention_decode(const moe_kv_cache* c, int32_t n_q_heads
   a.rows = sp.rows;
   a.items = sp.items;
   a.wave_heads = sp.wave_heads;
+  a.hts = sp.items / c->n_kv_heads;
   a.D = c->head_dim;
   a.window = opt->window;
   a.least = sp.least;
+  a.parts = sp.parts;
+  a.inverse_parts = 1.0 / sp.parts;
   a.scale = opt->scale;
   a.cap = opt->softcap;
   a.inv_cap = opt->softcap > 0.f ? 1.f / opt->softcap : 0.f;

@@ -34,26 +34,18 @@ inline PageDivisor page_divisor(int d) {
   return PageDivisor{(uint32_t)(((1ull << (31 + s)) + (uint64_t)d - 1) / (uint64_t)d), 31 + s};
 }
 
-// How attention splits over the length.  A sequence's kept places lie in tiles; `items` workgroups (key-value heads times tiles
-// of query heads) each work on every tile.  One size c of chunks for the whole batch, from the lengths alone: about `target`
-// workgroups in all, at least `least` tiles a chunk.  With c >= total*items/target the sum over the sequences of ceil(tiles/c)
-// is at most target/items + sequences, which is what the grid and the workspace are made for.
-MOESYS_HD int chunk_tiles(int64_t total_tiles, int items, int target, int least) {
-  const int64_t c = (total_tiles * items + target - 1) / target;
-  return c < least ? least : (int)c;
+// How attention deals the batch out.  The sequences' tiles stand in one row, sequence after sequence, an empty one as one tile
+// (somebody has to write its zeros); part w of the row is the tiles w*share .. (w+1)*share - 1.  A part holds pieces of one or more
+// sequences; a sequence that lies in one part is finished there, the pieces of the others are joined.
+MOESYS_HD int64_t row_tiles(int tiles) { return tiles > 0 ? tiles : 1; }
+// Tiles of a part: enough that `parts` of them hold the row (inverse = 1.0 / parts; floor + 1 is at least the quotient rounded up,
+// whichever way the product was rounded), at least `least`.
+MOESYS_HD int64_t share_of_row(int64_t total, double inverse, int least) {
+  const int64_t share = (int64_t)((double)total * inverse) + 1;
+  return share < least ? least : share;
 }
-// Chunks of a sequence (an empty one has one, which writes its zeros).
-MOESYS_HD int chunk_count(int tiles, int c) { return tiles <= c ? 1 : (tiles - 1) / c + 1; }
-// First tile of chunk j of n: even shares, the first ones one longer.
-MOESYS_HD int chunk_begin(int tiles, int n, int j) {
-  const int share = tiles / n, rest = tiles % n;
-  return j * share + (j < rest ? j : rest);
-}
-// The most chunks a batch can have, whatever its lengths.
-inline int64_t most_chunks(int64_t sequences, int items, int target, int least, int64_t tiles_per_sequence) {
-  const int64_t each = tiles_per_sequence <= least ? 1 : (tiles_per_sequence - 1) / least + 1;
-  const int64_t split = target / items + sequences;
-  return each * sequences < split ? each * sequences : split;
-}
+// Pieces that can be unfinished are a part's first and its last: two slots for each part, 2w for the first piece.  Slot of piece j of
+// a sequence whose first piece has slot `first`: it goes on as the first piece of the parts that follow.
+MOESYS_HD int piece_slot(int first, int j) { return j == 0 ? first : (first / 2 + j) * 2; }
 
 }  // namespace moesys

@@ -183,9 +183,9 @@ def test_places_on_the_host(tmp_path):
 }""")
 
 
-def test_pages_and_chunks_on_the_host(tmp_path):
-    """Page numbers by multiplication equal division; the chunks of a sequence cover its tiles once, in order; no batch has more
-    than the grid and the workspace are made for."""
+def test_pages_and_parts_on_the_host(tmp_path):
+    """Page numbers by multiplication equal division; the parts of a batch's row of tiles hold every tile once, and every
+    unfinished piece has a slot of its own where the join finds it."""
     compiled(tmp_path, """
 unsigned long long seed = 1;
 unsigned next() { seed = seed * 6364136223846793005ull + 1442695040888963407ull; return (unsigned)(seed >> 33); }
@@ -200,19 +200,41 @@ int main() {
   assert(kept_tiles(0, 0, 32) == 0 && kept_tiles(1, 0, 32) == 1 && kept_tiles(32, 0, 32) == 1 && kept_tiles(33, 0, 32) == 2);
   assert(kept_tiles(33, 31, 32) == 2 && kept_tiles(33, 32, 32) == 1 && kept_tiles(2147483647, 0, 32) == 67108864);
   for (int round = 0; round < 3000; ++round) {
-    const int items = 1 + next() % 300, target = 1 + next() % 2048, least = 1 + next() % 20, S = 1 + next() % 40;
-    const long long cap = 1 + next() % (round % 3 ? 200 : 100000);
-    std::vector<int> tiles(S);
-    long long total = 0, chunks = 0;
-    for (int& t : tiles) { t = next() % 5 ? (int)(next() % (cap + 1)) : 0; total += t; }
-    const int c = chunk_tiles(total, items, target, least);
-    for (int t : tiles) {
-      const int n = chunk_count(t, c);
-      chunks += n;
-      assert(n >= 1 && n <= target / items + 1 && chunk_begin(t, n, 0) == 0 && chunk_begin(t, n, n) == t);
-      for (int j = 0; j < n; ++j) { const int size = chunk_begin(t, n, j + 1) - chunk_begin(t, n, j); assert(size <= c && (size > 0 || t == 0)); }
+    const int parts = 1 + next() % (round % 2 ? 1000 : 7), least = 1 + next() % 20, S = 1 + next() % 40;
+    const long long cap = 1 + next() % (round % 3 ? 200 : 3000);
+    std::vector<long long> tiles(S);
+    long long total = 0;
+    for (long long& t : tiles) { t = row_tiles(next() % 5 ? (int)(next() % (cap + 1)) : 0); assert(t >= 1); total += t; }
+    const long long share = share_of_row(total, 1.0 / parts, least);
+    assert(share >= least && share * parts >= total);
+    // the parts walk over the row as the kernel does; every piece but whole ones has a slot of its own, where the join looks
+    std::vector<int> pieces(S, 0), first(S, -1), used(2 * parts, -1);
+    long long covered = 0;
+    for (int w = 0; w < parts; ++w) {
+      long long x = w * share, x_end = x + share < total ? x + share : total, begin = 0;
+      int b = 0;
+      if (x >= total) continue;
+      while (begin + tiles[b] <= x) begin += tiles[b++];
+      for (int no = 0; x < x_end; ++no) {
+        const long long b_end = begin + tiles[b], stop = b_end < x_end ? b_end : x_end;
+        const bool whole = x == begin && b_end <= x_end;
+        const int slot = 2 * w + (no > 0);
+        if (x == begin) {
+          first[b] = slot;
+          const int expected = whole ? 1 : (int)((b_end - 1) / share) - w + 1;
+          pieces[b] = -expected;
+        }
+        if (!whole) { assert(used[slot] < 0); used[slot] = b; }
+        const int j = w - first[b] / 2;
+        assert(first[b] >= 0 && piece_slot(first[b], j) == slot && j < -pieces[b]);
+        covered += stop - x;
+        if (b_end <= x_end) assert(j == -pieces[b] - 1);
+        x = b_end; begin = b_end; ++b;
+      }
     }
-    assert(chunks <= most_chunks(S, items, target, least, cap));
-    if (cap <= least) assert(chunks == S);
+    assert(covered == total);
   }
+  // the quotient in float64, at its worst
+  for (long long total : {1ll, 2ll, 3ll, 1000000007ll, (1ll << 40) - 1, 1ll << 40, (1ll << 40) + 1})
+    for (int parts = 1; parts < 3000; ++parts) assert(share_of_row(total, 1.0 / parts, 1) * parts >= total);
 }""")
