@@ -63,40 +63,39 @@ def _dtype(t) -> int:
     return _DTYPES[t.dtype]
 
 
-def _rows(t, what: str, shape, dtype) -> _HeadRows:
+def _rows(t, what: str, shape, dtype, device: int) -> _HeadRows:
     """[tokens, heads, head_dim] as the library takes it, checked against what the call says it holds."""
     if t.shape != shape:
         raise ValueError(f"{what} has shape {tuple(t.shape)}, the call needs {shape}")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise ValueError(f"{what} is {t.dtype}, the call needs {dtype}")
-    st, sh, sd = t.stride()
-    if sd != 1 and shape[2] > 1:
+    if t.get_device() != device:
+        _wrong_device(what, t, device)
+    token, head, element = t.stride()
+    if element != 1 and shape[2] > 1:
         raise ValueError(f"{what}: the elements of a head must be contiguous")
-    return _HeadRows(t.data_ptr(), st, sh)
+    return _HeadRows(t.data_ptr(), token, head)
 
 
-def _ints(t, what: str, *shapes) -> Optional[int]:
-    """A contiguous int32 tensor of one of the given shapes."""
+def _vector(t, what: str, dtype, shape, device: int) -> Optional[int]:
+    """The address of a contiguous tensor of a shape and dtype."""
     if t is None:
         return None
-    if t.dtype != torch.int32 or tuple(t.shape) not in shapes or not t.is_contiguous():
-        raise ValueError(f"{what} is a {t.dtype} tensor of shape {tuple(t.shape)}, the call needs a contiguous int32 one of {' or '.join(map(str, shapes))}")
+    if t.shape != shape or t.dtype is not dtype or not t.is_contiguous():
+        raise ValueError(f"{what} is a {t.dtype} tensor of shape {tuple(t.shape)}, the call needs a contiguous {dtype} one of shape {shape}")
+    if t.get_device() != device:
+        _wrong_device(what, t, device)
     return t.data_ptr()
 
 
-def _on_device(*tensors) -> int:
-    """The one CUDA device that all of the tensors are on."""
-    device = -1
-    for t in tensors:
-        if t is None:
-            continue
-        d = t.get_device()
-        if d < 0:
-            raise ValueError("device tensors are needed")
-        if device < 0:
-            device = d
-        elif d != device:
-            raise ValueError(f"tensors on CUDA devices {device} and {d}")
+def _wrong_device(what: str, t, device: int) -> None:
+    raise ValueError(f"{what} is on {t.device}: device tensors are needed" + (f", here on CUDA device {device}" if device >= 0 else ""))
+
+
+def _device(t, what: str) -> int:
+    device = t.get_device()
+    if device < 0:
+        _wrong_device(what, t, device)
     return device
 
 
@@ -113,7 +112,7 @@ class Rotary:
     def __init__(self, head_dim: int, freqs, axis_pairs: Optional[Sequence[int]] = None, interleaved: bool = False):
         if freqs.dtype != torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous():
             raise ValueError("freqs must be a contiguous float64 vector")
-        _on_device(freqs)
+        self.device = _device(freqs, "freqs")
         pairs = [freqs.numel()] if axis_pairs is None else [int(n) for n in axis_pairs]
         if not 1 <= len(pairs) <= _MAX_AXES:
             raise ValueError(f"{len(pairs)} axes: 1 to {_MAX_AXES} are supported")
@@ -143,51 +142,68 @@ class KVCache:
             raise ValueError("the elements of a head must be contiguous")
         if page_table.dtype != torch.int32 or page_table.dim() != 2 or not page_table.is_contiguous():
             raise ValueError("page_table must be a contiguous int32 matrix")
-        _on_device(k, v, page_table)
+        self.device = _device(k, "k")
+        for t, what in ((v, "v"), (page_table, "page_table")):
+            if t.get_device() != self.device:
+                _wrong_device(what, t, self.device)
         self.k, self.v, self.page_table, self.layout = k, v, page_table, layout
         tok, head = (1, 2) if layout == "token_major" else (2, 1)
         self.page_size, self.n_kv_heads, self.head_dim = k.shape[tok], k.shape[head], k.shape[3]
         self.n_seqs, self.dtype = page_table.shape[0], k.dtype
+        self.scale = self.head_dim ** -0.5
         self.c = _Cache(k.data_ptr() or None, v.data_ptr() or None, page_table.data_ptr() or None, k.shape[0], k.stride(0), k.stride(tok),
                         k.stride(head), self.page_size, page_table.shape[0], page_table.shape[1], self.n_kv_heads, self.head_dim, _dtype(k))
         B._check(lib().moe_kv_cache_check(C.byref(self.c)), "moe_kv_cache_check")
 
 
 def moe_rotary(rotary: Rotary, x, positions, out, inverse: bool = False, stream=None):
-    """out <- x [T, heads, head_dim] rotated by positions [axes, T] (int32); ``inverse``: back, or the gradient."""
-    T, H, D = x.shape
-    device = _on_device(x, positions, out, rotary.freqs)
+    """out <- x [T, heads, head_dim] rotated by positions [axes, T] (int32; [T] for one axis); ``inverse``: back, or the gradient."""
+    shape, dtype, device = tuple(x.shape), x.dtype, rotary.device
+    T, H, D = shape
     if D != rotary.head_dim:
         raise ValueError(f"x has heads of {D}, the rotary positions are for {rotary.head_dim}")
-    xr, outr = _rows(x, "x", (T, H, D), x.dtype), _rows(out, "out", (T, H, D), x.dtype)
-    pos = _ints(positions, "positions", (rotary.n_axes, T), *([(T,)] if rotary.n_axes == 1 else []))
-    B._check(lib().moe_rotary(C.byref(rotary.c), _dtype(x), T, H, C.byref(xr), pos, C.byref(outr), int(bool(inverse)), _stream(stream, device)), "moe_rotary")
+    st = lib().moe_rotary(rotary.c, _dtype(x), T, H, _rows(x, "x", shape, dtype, device), _positions(rotary, positions, T, device),
+                          _rows(out, "out", shape, dtype, device), 1 if inverse else 0, _stream(stream, device))
+    if st:
+        B._check(st, "moe_rotary")
+
+
+def _positions(rotary: Rotary, positions, T: int, device: int) -> int:
+    shape = (T,) if positions.dim() == 1 and rotary.n_axes == 1 else (rotary.n_axes, T)
+    return _vector(positions, "positions", torch.int32, shape, device)
 
 
 def moe_kv_append(cache: KVCache, k, v, cache_pos, token_seq=None, rotary: Optional[Rotary] = None, positions=None, q=None, q_out=None,
                   stream=None):
     """Keys and values [T, kv_heads, head_dim] of new tokens into their places of the cache, keys rotated; queries
     [T, heads, head_dim] rotated into q_out."""
-    T = k.shape[0]
-    device = _on_device(k, v, cache_pos, token_seq, positions, q, q_out, cache.k, rotary.freqs if rotary is not None else None)
-    kv = (T, cache.n_kv_heads, cache.head_dim)
-    kr, vr = _rows(k, "k", kv, cache.dtype), _rows(v, "v", kv, cache.dtype)
-    qr = qo = None
-    hq = 0
+    T, D, dtype, device = k.shape[0], cache.head_dim, cache.dtype, cache.device
+    shape, per_token = (T, cache.n_kv_heads, D), (T,)
+    spec = pos = q_rows = q_out_rows = None
+    heads = 0
+    if rotary is not None:
+        if rotary.device != device:
+            raise ValueError(f"rotary positions of CUDA device {rotary.device}, a cache on {device}")
+        spec = rotary.c
+        if positions is not None:
+            pos = _positions(rotary, positions, T, device)
+    elif positions is not None:
+        raise ValueError("positions without rotary")
     if q is not None:
         if q_out is None:
             raise ValueError("q without q_out")
-        hq = q.shape[1]
-        qr, qo = _rows(q, "q", (T, hq, cache.head_dim), cache.dtype), _rows(q_out, "q_out", (T, hq, cache.head_dim), cache.dtype)
-    axes = rotary.n_axes if rotary is not None else 1
-    B._check(lib().moe_kv_append(
-        C.byref(cache.c), T, C.byref(kr), C.byref(vr), _ints(token_seq, "token_seq", (T,)), _ints(cache_pos, "cache_pos", (T,)),
-        C.byref(rotary.c) if rotary is not None else None, _ints(positions, "positions", (axes, T), *([(T,)] if axes == 1 else [])), hq,
-        C.byref(qr) if qr is not None else None, C.byref(qo) if qo is not None else None, _stream(stream, device)), "moe_kv_append")
+        heads = q.shape[1]
+        q_shape = (T, heads, D)
+        q_rows, q_out_rows = _rows(q, "q", q_shape, dtype, device), _rows(q_out, "q_out", q_shape, dtype, device)
+    st = lib().moe_kv_append(cache.c, T, _rows(k, "k", shape, dtype, device), _rows(v, "v", shape, dtype, device),
+                             _vector(token_seq, "token_seq", torch.int32, per_token, device), _vector(cache_pos, "cache_pos", torch.int32, per_token, device),
+                             spec, pos, heads, q_rows, q_out_rows, _stream(stream, device))
+    if st:
+        B._check(st, "moe_kv_append")
 
 
 def moe_attention_decode_workspace_bytes(cache: KVCache, n_q_heads: int) -> int:
-    n = lib().moe_attention_decode_workspace_bytes(C.byref(cache.c), n_q_heads)
+    n = lib().moe_attention_decode_workspace_bytes(cache.c, n_q_heads)
     if n == 0:
         raise B.MoEError(1, "moe_attention_decode_workspace_bytes", lib().moe_last_error().decode())
     return n
@@ -197,15 +213,13 @@ def moe_attention_decode(cache: KVCache, q, seq_lens, out, ws, scale: Optional[f
                          slopes=None, lse=None, stream=None):
     """Attention of one new token per sequence: q, out [sequences, heads, head_dim], seq_lens int32 [sequences] (the new token
     counted), slopes float32 [heads] (optional), lse float32 [sequences, heads] (optional output)."""
-    S, H, D = cache.n_seqs, q.shape[1], cache.head_dim
-    device = _on_device(q, seq_lens, out, ws, slopes, lse, cache.k)
-    qr, outr = _rows(q, "q", (S, H, D), cache.dtype), _rows(out, "out", (S, H, D), cache.dtype)
-    for t, what, shape in ((slopes, "slopes", (H,)), (lse, "lse", (S, H))):
-        if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous()):
-            raise ValueError(f"{what} must be a contiguous float32 tensor of shape {shape}")
-    if not ws.is_contiguous():
-        raise ValueError("the workspace must be contiguous")
-    opt = _Options(D ** -0.5 if scale is None else scale, softcap, window, slopes.data_ptr() if slopes is not None else None)
-    B._check(lib().moe_attention_decode(
-        C.byref(cache.c), H, C.byref(qr), _ints(seq_lens, "seq_lens", (S,)), C.byref(opt), C.byref(outr), lse.data_ptr() if lse is not None else None,
-        ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream, device)), "moe_attention_decode")
+    S, H, dtype, device = cache.n_seqs, q.shape[1], cache.dtype, cache.device
+    shape = (S, H, cache.head_dim)
+    if not ws.is_contiguous() or ws.get_device() != device:
+        raise ValueError("the workspace must be contiguous and on the cache's device")
+    options = _Options(cache.scale if scale is None else scale, softcap, window, _vector(slopes, "slopes", torch.float32, (H,), device))
+    st = lib().moe_attention_decode(cache.c, H, _rows(q, "q", shape, dtype, device), _vector(seq_lens, "seq_lens", torch.int32, (S,), device), options,
+                                    _rows(out, "out", shape, dtype, device), _vector(lse, "lse", torch.float32, (S, H), device),
+                                    ws.data_ptr(), ws.nbytes, _stream(stream, device))
+    if st:
+        B._check(st, "moe_attention_decode")

@@ -22,6 +22,7 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -39,7 +40,7 @@ __device__ const u32x4 ZEROS[MOE_MAX_HEAD_DIM * 4 / 16] = {};
 // Workgroups of the decode kernel that a CU holds: two need up to 256 registers a lane, which keys and values of 128 dimensions on
 // their way leave room for; a third or a fourth costs registers for what is in flight (64 sequences, 1.3 GB: 210 us with two,
 // 237 with three), and 256 dimensions need more than 256 (130 MB: 48 us with one, 64 with two, which spill).
-constexpr int resident_workgroups(int dims) { return dims <= 128 ? 2 : 1; }
+constexpr int resident_workgroups(int dims, int elem) { return dims <= 128 || elem == 2 ? 2 : 1; }
 
 struct DecodeArgs {
   const char *k, *v, *q;
@@ -52,14 +53,14 @@ struct DecodeArgs {
   int2* plan;      // [sequence]: slot of the first piece, pieces
   int64_t n_pages, page_stride, token_stride, head_stride, q_token, q_head, o_token, o_head;  // bytes
   PageDivisor page;
-  int32_t page_size, table_width, n_seqs, hq, hkv, G, rows, items, hts, wave_heads, parts, D, window, least;
+  int32_t page_size, table_width, n_seqs, hq, hkv, G, rows, items, hts, wave_heads, parts, one_each, D, window, least;
   float scale, cap, inv_cap;
   double inverse_parts;
 };
 
 template <typename X, int DP> struct Shape;
 template <int DP> struct Shape<__bf16, DP> {
-  static constexpr int SUB = 2, EPL = DP < 128 ? 4 : 8, KSTEPS = DP / 32;
+  static constexpr int SUB = DP <= 128 ? 2 : 1, EPL = DP < 128 ? 4 : 8, KSTEPS = DP / 32;
 };
 template <int DP> struct Shape<float, DP> {
   static constexpr int SUB = 1, EPL = 4, KSTEPS = DP / 16;
@@ -84,6 +85,7 @@ struct Position {
 __device__ __forceinline__ int length_of(const DecodeArgs& a, int b) { return kept_length(a.lens[b], a.table_width * a.page_size); }
 __device__ __forceinline__ Position find_part(const DecodeArgs& a, int tile, int w) {
   const int lane = threadIdx.x & 63;
+  if (a.one_each) return Position{1, a.n_seqs, w, w, length_of(a, w)};
   auto in_row = [&](int n) { return row_tiles(kept_tiles(n, first_place(n, a.window), tile)); };
   int n = lane < a.n_seqs ? length_of(a, lane) : 0;
   int64_t mine = lane < a.n_seqs ? in_row(n) : 0, total = mine;
@@ -139,6 +141,15 @@ __device__ __forceinline__ f32x4 product(const u32x4& a, const u32x4& b, f32x4 a
   }
 }
 
+// acc + a b over the places of a tile, 8 (two subtiles) or 4 of them per lane as pairs of bfloat16
+template <int SUB>
+__device__ __forceinline__ f32x4 weighted(const uint32_t (&a)[2 * SUB], const uint32_t (&b)[2 * SUB], f32x4 acc) {
+  if constexpr (SUB == 2)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, (u32x4{a[0], a[1], a[2], a[3]})), __builtin_bit_cast(bf16x8, (u32x4{b[0], b[1], b[2], b[3]})), acc, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(i16x4, (u32x2{a[0], a[1]})), __builtin_bit_cast(i16x4, (u32x2{b[0], b[1]})), acc, 0, 0, 0);
+}
+
 // What the lane 32 away holds.
 __device__ __forceinline__ float other_half(float x, int lane) {
   const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -159,7 +170,7 @@ __device__ __forceinline__ void store_row(const DecodeArgs& a, int b, int h, int
 // One (sequence, kv head, tile of query heads, chunk of places) per workgroup; its wavefronts take the chunk's tiles in turn.
 // FULL: head_dim is DP, no lane's dimensions lie beyond it.
 template <typename X, int DP, bool FULL, bool NT>
-__global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP)) void decode_kernel(DecodeArgs a) {
+__global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) void decode_kernel(DecodeArgs a) {
   using S = Shape<X, DP>;
   constexpr bool BF16 = sizeof(X) == 2;
   constexpr int SUB = S::SUB, TILE = 16 * SUB, EPL = S::EPL, KSTEPS = S::KSTEPS, LINES = KSTEPS / 2, NV = 4 * SUB, BD = 16 * EPL, NBLK = DP / BD, PITCH = BD + 4;
@@ -190,8 +201,8 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP)) void decode_ke
   // the piece of sequence b that lies in this part
   const int b = at.b;
   const int n = at.n, first = first_place(n, a.window), tile0 = first / TILE, tiles = kept_tiles(n, first, TILE);
-  const int64_t b_end = at.begin + row_tiles(tiles);
-  const int from = (int)(x - at.begin), upto = b_end < x_end ? tiles : (int)(x_end - at.begin);
+  const int64_t b_end = at.begin + (a.one_each ? 1 : row_tiles(tiles));
+  const int from = (int)(x - at.begin), upto = b_end <= x_end ? tiles : (int)(x_end - at.begin);
   const bool whole = from == 0 && b_end <= x_end;
   const int slot = 2 * w + (piece_no > 0);
   if (from == 0 && threadIdx.x == 0 && item == 0)
@@ -346,26 +357,23 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP)) void decode_ke
     if constexpr (BF16) {
       // A weight enters as the sum of two bfloat16 numbers, 16 bits of mantissa: one alone would add half of the output's own
       // rounding to its error, and the matrix units are idle most of the time.
-      uint32_t hi[4], lo[4];
+      uint32_t hi[2 * SUB], lo[2 * SUB];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < 2 * SUB; ++i) {
         const float p0 = z[i / 2][i % 2 * 2], p1 = z[i / 2][i % 2 * 2 + 1];
         hi[i] = pack_bf16(p0, p1);
         lo[i] = pack_bf16(p0 - __uint_as_float(hi[i] << 16), p1 - __uint_as_float(hi[i] & 0xffff0000u));
       }
-      const bf16x8 ph = __builtin_bit_cast(bf16x8, (u32x4{hi[0], hi[1], hi[2], hi[3]}));
-      const bf16x8 pl = __builtin_bit_cast(bf16x8, (u32x4{lo[0], lo[1], lo[2], lo[3]}));
 #pragma unroll
       for (int blk = 0; blk < NBLK; ++blk)
 #pragma unroll
         for (int j = 0; j < EPL; ++j) {
-          u32x4 w;
+          uint32_t vt[2 * SUB];
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            w[i] = __builtin_amdgcn_perm(vr[2 * i + 1][blk][j / 2], vr[2 * i][blk][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
-          const bf16x8 vt = __builtin_bit_cast(bf16x8, w);
-          o[blk][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, ph, o[blk][j], 0, 0, 0);
-          o[blk][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pl, o[blk][j], 0, 0, 0);
+          for (int i = 0; i < 2 * SUB; ++i)
+            vt[i] = __builtin_amdgcn_perm(vr[2 * i + 1][blk][j / 2], vr[2 * i][blk][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+          o[blk][j] = weighted<SUB>(vt, hi, o[blk][j]);
+          o[blk][j] = weighted<SUB>(vt, lo, o[blk][j]);
         }
     } else {
 #pragma unroll
@@ -512,30 +520,37 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(DecodeArgs a) {
 // The split of a call: what its grid, its workspace and its kernels agree on.
 struct Split {
   int rows, items, wave_heads, least, parts;
-  bool nt;
+  bool nt, one_each;
   size_t ml, o, total;  // bytes: offsets of the pieces (the plan lies in front)
 };
 
 Split split_of(const moe_kv_cache* c, int32_t n_q_heads) {
   Split s;
-  const int G = n_q_heads / c->n_kv_heads, tile = c->dtype == MOE_BF16 ? 32 : 16;
+  const int G = n_q_heads / c->n_kv_heads, tile = c->dtype == MOE_BF16 && c->head_dim <= 128 ? 32 : 16;
   s.rows = G < HEADS ? G : HEADS;
   s.items = c->n_kv_heads * ((G + HEADS - 1) / HEADS);
+  const int64_t capacity = (int64_t)c->table_width * c->page_size, tiles = (capacity + tile - 1) / tile;
+  // Short sequences stay whole: no second launch, and no search for a part.  Measured: one sequence of 173 places 6.8 us whole and
+  // 12.1 split, of 1000 places 15.0 and 13.8; 16 of up to 1000 places 15.4 and 18.1, 512 of up to 700 131 and 140; 256 of up to 2000
+  // 186 and 171.
+  s.one_each = capacity <= ((int64_t)c->n_seqs * s.items >= 128 ? 1024 : 512);
   // Neighbouring items by one workgroup: tiles of query heads that read the same keys and values, and kv heads whose rows are
   // neighbours in memory.
-  const bool several = s.items > c->n_kv_heads, neighbours = c->head_stride < c->token_stride;
+  const bool several = s.items > c->n_kv_heads, neighbours = c->head_stride < c->token_stride && !s.one_each;
   const int wanted = several ? 4 : !neighbours ? 1 : c->head_dim * (int)elem_size(c->dtype) <= 128 ? 4 : 2;
   s.wave_heads = s.items % wanted == 0 ? wanted : s.items % 2 == 0 && wanted > 1 ? 2 : 1;
   s.least = LEAST_PER_WAVE * WAVES / s.wave_heads;
-  const int64_t tiles = ((int64_t)c->table_width * c->page_size + tile - 1) / tile, groups = s.items / s.wave_heads;
-  const int64_t resident = 256 * resident_workgroups(c->head_dim) / groups;
+  const int64_t resident = 256 * resident_workgroups(c->head_dim, (int)elem_size(c->dtype)) / (s.items / s.wave_heads);
   const int64_t most = (c->n_seqs * (tiles > 0 ? tiles : 1) + s.least - 1) / s.least;
   s.parts = (int)(most < resident ? most : resident);
   if (s.parts < 1) s.parts = 1;
+  if (s.one_each) s.parts = c->n_seqs;
   s.nt = (double)c->n_pages * c->page_size * c->n_kv_heads * c->head_dim * 2 * elem_size(c->dtype) > (double)(300 << 20);
   s.ml = align_up((size_t)c->n_seqs * sizeof(int2), 256);
-  s.o = s.ml + align_up((size_t)s.parts * 2 * s.items * s.rows * sizeof(f32x2), 256);
-  s.total = s.o + align_up((size_t)s.parts * 2 * s.items * s.rows * c->head_dim * sizeof(float), 256);
+  const size_t slots = s.one_each ? 0 : (size_t)s.parts * 2;
+  s.o = s.ml + align_up(slots * s.items * s.rows * sizeof(f32x2), 256);
+  s.total = s.o + align_up(slots * s.items * s.rows * c->head_dim * sizeof(float), 256);
+  if (s.total < 256) s.total = 256;
   return s;
 }
 
@@ -554,12 +569,12 @@ void launch(const DecodeArgs& a, unsigned grid, bool nt, hipStream_t s) {
 
 template <typename X>
 int32_t launch_decode(const DecodeArgs& a, const Split& sp, hipStream_t s) {
-  const unsigned grid = (unsigned)(sp.parts * (sp.items / sp.wave_heads));
+  const unsigned grid = (unsigned)((int64_t)sp.parts * (sp.items / sp.wave_heads));
   if (a.D <= 64) launch<X, 64>(a, grid, sp.nt, s);
   else if (a.D <= 128) launch<X, 128>(a, grid, sp.nt, s);
   else launch<X, 256>(a, grid, sp.nt, s);
   int32_t st = check_hip(hipGetLastError(), "attention launch");
-  if (st != MOE_OK || sp.parts == 1) return st;  // (every sequence was finished)
+  if (st != MOE_OK || sp.one_each) return st;
   const int64_t rows = (int64_t)a.n_seqs * a.hq;
   // (a row has about parts / sequences pieces; the weights of four rows' take LDS)
   if (rows >= MANY_ROWS) {
@@ -641,6 +656,7 @@ extern "C" int32_t moe_attention_decode(const moe_kv_cache* c, int32_t n_q_heads
   a.window = opt->window;
   a.least = sp.least;
   a.parts = sp.parts;
+  a.one_each = sp.one_each;
   a.inverse_parts = 1.0 / sp.parts;
   a.scale = opt->scale;
   a.cap = opt->softcap;

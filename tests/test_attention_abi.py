@@ -155,15 +155,19 @@ def test_binding_refuses():
         M.Rotary(64, torch.zeros(32, dtype=torch.float64))
     x = torch.zeros(3, 2, 64)
     with pytest.raises(ValueError, match="shape"):
-        B._rows(x, "x", (3, 2, 32), torch.float32)
+        B._rows(x, "x", (3, 2, 32), torch.float32, -1)
     with pytest.raises(ValueError, match="bfloat16"):
-        B._rows(x, "x", (3, 2, 64), torch.bfloat16)
+        B._rows(x, "x", (3, 2, 64), torch.bfloat16, -1)
     with pytest.raises(ValueError, match="contiguous"):
-        B._rows(x.transpose(1, 2), "x", (3, 64, 2), torch.float32)
+        B._rows(x.transpose(1, 2), "x", (3, 64, 2), torch.float32, -1)
     with pytest.raises(ValueError, match="int32"):
-        B._ints(torch.zeros(3), "seq_lens", (3,))
+        B._vector(torch.zeros(3), "seq_lens", torch.int32, (3,), -1)
     with pytest.raises(ValueError, match="int32"):
-        B._ints(torch.zeros(4, dtype=torch.int32), "seq_lens", (3,))
+        B._vector(torch.zeros(4, dtype=torch.int32), "seq_lens", torch.int32, (3,), -1)
+    with pytest.raises(ValueError, match="device tensors"):
+        B._vector(torch.zeros(3, dtype=torch.int32), "seq_lens", torch.int32, (3,), 0)
+    with pytest.raises(ValueError, match="device tensors"):
+        B._rows(x, "x", (3, 2, 64), torch.float32, 0)
 
 
 # ---- places, on the host -----------------------------------------------------------------------------------
