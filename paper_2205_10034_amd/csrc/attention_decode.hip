@@ -30,7 +30,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int WAVES = 4;
 constexpr int HEADS = 16;  // query heads of a tile
-constexpr int LEAST_PER_WAVE = 2, MANY_ROWS = 1024;
+constexpr int LEAST_PER_WAVE = 2, MANY_ROWS = 1024, TINY_PLACES = 128, SMALL_PLACES = 1024;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 // Rows of places that are not there and dimensions beyond head_dim are read from here: no load leaves the caller's rows, and what
@@ -53,9 +53,8 @@ struct DecodeArgs {
   int2* plan;      // [sequence]: slot of the first piece, pieces
   int64_t n_pages, page_stride, token_stride, head_stride, q_token, q_head, o_token, o_head;  // bytes
   PageDivisor page;
-  int32_t page_size, table_width, n_seqs, hq, hkv, G, rows, items, hts, wave_heads, parts, one_each, D, window, least;
+  int32_t page_size, table_width, n_seqs, hq, hkv, G, rows, items, hts, wave_heads, parts, may_split, D, window, least;
   float scale, cap, inv_cap;
-  double inverse_parts;
 };
 
 template <typename X, int DP> struct Shape;
@@ -70,31 +69,64 @@ template <int BYTES> struct Words;
 template <> struct Words<8> { typedef u32x2 type; };
 template <> struct Words<16> { typedef u32x4 type; };
 
+// How many of the neighbouring items one workgroup takes so that the `rows` fit `grid` workgroups, if they can.
+__device__ __forceinline__ int side_by_side(int items, int64_t rows, int64_t grid) {
+  return rows <= grid || items % 2 ? 1 : rows <= 2 * grid || items % 4 ? 2 : 4;
+}
+
 // A value that all lanes hold, for the scalar registers.
 __device__ __forceinline__ int64_t uniform(int64_t v, int lane) {
   const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)v, lane), hi = __builtin_amdgcn_readlane((int)(v >> 32), lane);
   return (int64_t)(((uint64_t)hi << 32) | lo);
 }
 
-// Where part `w` of the row of tiles begins; every wavefront finds it by itself.
-struct Position {
-  int64_t share, total;  // tiles of a part, of the row
-  int64_t begin;         // the sequence's first tile in the row
-  int b, n;              // sequence, its kept length
+// How the workgroups share the batch, from its lengths: a wavefront's place in it.  Every wavefront finds it by itself.
+struct Deal {
+  int wave_heads, groups, w;  // items of a workgroup, workgroups that share a part, the part
+  bool one_each;              // the row counts sequences, not tiles: no sequence is split
+  int64_t share, total;       // of a part, of the row
+  int64_t begin;              // where in the row sequence b begins
+  int b, n;                   // the part's first sequence, its kept length
 };
 __device__ __forceinline__ int length_of(const DecodeArgs& a, int b) { return kept_length(a.lens[b], a.table_width * a.page_size); }
-__device__ __forceinline__ Position find_part(const DecodeArgs& a, int tile, int w) {
-  const int lane = threadIdx.x & 63;
-  if (a.one_each) return Position{1, a.n_seqs, w, w, length_of(a, w)};
-  auto in_row = [&](int n) { return row_tiles(kept_tiles(n, first_place(n, a.window), tile)); };
-  int n = lane < a.n_seqs ? length_of(a, lane) : 0;
-  int64_t mine = lane < a.n_seqs ? in_row(n) : 0, total = mine;
-  for (int s = lane + 64; s < a.n_seqs; s += 64) total += in_row(length_of(a, s));
+
+__device__ __forceinline__ Deal deal(const DecodeArgs& a, int tile) {
+  const int lane = threadIdx.x & 63, id = blockIdx.x;
+  auto tiles_in = [&](int n) { return kept_tiles(n, first_place(n, a.window), tile); };
+  const int64_t rows = (int64_t)a.n_seqs * a.items, grid = gridDim.x;
+  Deal p{};
+  auto take = [&](int wave_heads) {
+    p.wave_heads = wave_heads;
+    p.groups = a.items / wave_heads;
+    p.w = id / p.groups;
+    return (int)grid / p.groups;  // parts
+  };
+  auto whole = [&] {
+    const int parts = take(side_by_side(a.items, rows, grid));
+    p.one_each = true;
+    p.share = (a.n_seqs + parts - 1) / parts;
+    p.total = a.n_seqs;
+    p.begin = p.w * p.share;
+    p.b = (int)p.begin;
+    if (p.begin < p.total) p.n = length_of(a, p.b);
+    return p;
+  };
+  if (!a.may_split) return whole();
+  int n = lane < a.n_seqs ? length_of(a, lane) : 0, longest = tiles_in(n);
+  int64_t mine = lane < a.n_seqs ? row_tiles(longest) : 0, total = mine;
+  for (int s = lane + 64; s < a.n_seqs; s += 64) {
+    const int t = tiles_in(length_of(a, s));
+    longest = t > longest ? t : longest;
+    total += row_tiles(t);
+  }
+  const bool tiny = !__any(longest > TINY_PLACES / tile), small = !__any(longest > SMALL_PLACES / tile);
+  if (tiny || (small && rows <= grid)) return whole();
   for (int d = 1; d < 64 && d < a.n_seqs; d <<= 1) total += __shfl_xor(total, d, 64);
-  total = uniform(total, 0);
-  Position p{uniform(share_of_row(total, a.inverse_parts, a.least), 0), total, 0, 0, 0};
-  const int64_t at = w * p.share;
-  if (at >= total) return p;
+  p.total = uniform(total, 0);
+  const int parts = take(p.total * tile < (int64_t)a.n_seqs * SMALL_PLACES && rows >= 2 * grid ? side_by_side(a.items, rows, grid) : a.wave_heads);
+  p.share = uniform(share_of_row(p.total, 1.0 / parts, a.least / p.wave_heads), 0);
+  const int64_t at = p.w * p.share;
+  if (at >= p.total) return p;
   for (int s = 0;;) {
     int64_t upto = mine;
     for (int d = 1; d < 64 && d < a.n_seqs; d <<= 1) {
@@ -112,7 +144,7 @@ __device__ __forceinline__ Position find_part(const DecodeArgs& a, int tile, int
     p.begin += uniform(upto, 63);
     s += 64;
     n = s + lane < a.n_seqs ? length_of(a, s + lane) : 0;
-    mine = s + lane < a.n_seqs ? in_row(n) : 0;
+    mine = s + lane < a.n_seqs ? row_tiles(tiles_in(n)) : 0;
   }
 }
 
@@ -182,9 +214,13 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) voi
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m16 = lane & 15, g = lane >> 4, piece = (g + 4 * (m16 >> 3)) * 16;
-  // wavefronts of a workgroup: wave_heads neighbouring kv heads, `step` of them on the tiles of each in turn
-  const int groups = a.items / a.wave_heads, w = blockIdx.x / groups, step = WAVES / a.wave_heads;
-  const int item = blockIdx.x % groups * a.wave_heads + wave % a.wave_heads, hk = item / a.hts, ht = item % a.hts;
+  // wavefronts of a workgroup: wave_heads neighbouring items, `step` of them on the tiles of each in turn
+  Deal at = deal(a, TILE);
+  const int wave_heads = at.wave_heads, w = at.w, step = WAVES / wave_heads;
+  int64_t x = w * at.share;
+  const int64_t x_end = x + at.share < at.total ? x + at.share : at.total;
+  if (x >= x_end) return;
+  const int item = blockIdx.x % at.groups * wave_heads + wave % wave_heads, hk = item / a.hts, ht = item % a.hts;
   auto heads_of = [&](int tile_of_heads) { return a.G - tile_of_heads * HEADS < HEADS ? a.G - tile_of_heads * HEADS : HEADS; };
   const int my_heads = heads_of(ht);
   const char* zeros = reinterpret_cast<const char*>(ZEROS);
@@ -194,21 +230,18 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) voi
   const float scale2 = a.scale * LOG2E;
   const float slope = a.slopes && m16 < my_heads ? a.slopes[hk * a.G + ht * HEADS + m16] : 0.f;
 
-  Position at = find_part(a, TILE, w);
-  int64_t x = w * at.share;
-  const int64_t x_end = x + at.share < at.total ? x + at.share : at.total;
   for (int piece_no = 0; x < x_end; ++piece_no) {
   // the piece of sequence b that lies in this part
   const int b = at.b;
   const int n = at.n, first = first_place(n, a.window), tile0 = first / TILE, tiles = kept_tiles(n, first, TILE);
-  const int64_t b_end = at.begin + (a.one_each ? 1 : row_tiles(tiles));
+  const int64_t b_end = at.begin + (at.one_each ? 1 : row_tiles(tiles));
   const int from = (int)(x - at.begin), upto = b_end <= x_end ? tiles : (int)(x_end - at.begin);
   const bool whole = from == 0 && b_end <= x_end;
   const int slot = 2 * w + (piece_no > 0);
   if (from == 0 && threadIdx.x == 0 && item == 0)
     a.plan[b] = make_int2(slot, whole ? 1 : (int)((b_end - 1) / at.share) - w + 1);
   const int t_end = tiles ? tile0 + upto : 0;
-  int t = tile0 + from + wave / a.wave_heads;
+  int t = tile0 + from + wave / wave_heads;
   const int32_t* table = a.table + (int64_t)b * a.table_width;
 
   // Nothing in the loop that loads is conditional: what a tile beyond the last one would load is ZEROS.  (Behind a branch the
@@ -398,7 +431,7 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) voi
   // (wavefront w and those a multiple of wave_heads away have the same kv head)
   auto joined_max = [&](int w, int row) {
     float top = -INFINITY;
-    for (w %= a.wave_heads; w < WAVES; w += a.wave_heads) top = fmaxf(top, ml_lds[w][row][0]);
+    for (w %= wave_heads; w < WAVES; w += wave_heads) top = fmaxf(top, ml_lds[w][row][0]);
     return top;
   };
   auto part_weight = [&](int w, int row, float top) { return top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml_lds[w][row][0] - top); };
@@ -418,13 +451,13 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) voi
     }
     lds_barrier();
     const int dim = blk * BD + d;
-    for (int i = threadIdx.x / (BD / 4); i < a.rows * a.wave_heads; i += 64 * WAVES / (BD / 4)) {
-      const int wh = i / a.rows, r = i % a.rows, its = item - wave % a.wave_heads + wh;  // the row's item
+    for (int i = threadIdx.x / (BD / 4); i < a.rows * wave_heads; i += 64 * WAVES / (BD / 4)) {
+      const int wh = i / a.rows, r = i % a.rows, its = item - wave % wave_heads + wh;  // the row's item
       if (r >= heads_of(its % a.hts)) continue;
       const float top = joined_max(wh, r);
       float sum = 0.f;
       f32x4 y{0.f, 0.f, 0.f, 0.f};
-      for (int w = wh; w < WAVES; w += a.wave_heads) {
+      for (int w = wh; w < WAVES; w += wave_heads) {
         sum += ml_lds[w][r][1] * part_weight(w, r, top);
         y += *reinterpret_cast<const f32x4*>(o_lds + (w * a.rows + r) * PITCH + d);
       }
@@ -519,38 +552,37 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(DecodeArgs a) {
 
 // The split of a call: what its grid, its workspace and its kernels agree on.
 struct Split {
-  int rows, items, wave_heads, least, parts;
-  bool nt, one_each;
+  int rows, items, wave_heads, least, grid, parts;
+  bool nt, join;
   size_t ml, o, total;  // bytes: offsets of the pieces (the plan lies in front)
 };
 
-Split split_of(const moe_kv_cache* c, int32_t n_q_heads) {
+Split split_of(const moe_kv_cache* c, int32_t n_q_heads, int32_t window) {
   Split s;
-  const int G = n_q_heads / c->n_kv_heads, tile = c->dtype == MOE_BF16 && c->head_dim <= 128 ? 32 : 16;
+  const int G = n_q_heads / c->n_kv_heads, es = (int)elem_size(c->dtype), tile = es == 2 && c->head_dim <= 128 ? 32 : 16;
   s.rows = G < HEADS ? G : HEADS;
   s.items = c->n_kv_heads * ((G + HEADS - 1) / HEADS);
-  const int64_t capacity = (int64_t)c->table_width * c->page_size, tiles = (capacity + tile - 1) / tile;
-  // Short sequences stay whole: no second launch, and no search for a part.  Measured: one sequence of 173 places 6.8 us whole and
-  // 12.1 split, of 1000 places 15.0 and 13.8; 16 of up to 1000 places 15.4 and 18.1, 512 of up to 700 131 and 140; 256 of up to 2000
-  // 186 and 171.
-  s.one_each = capacity <= ((int64_t)c->n_seqs * s.items >= 128 ? 1024 : 512);
   // Neighbouring items by one workgroup: tiles of query heads that read the same keys and values, and kv heads whose rows are
   // neighbours in memory.
-  const bool several = s.items > c->n_kv_heads, neighbours = c->head_stride < c->token_stride && !s.one_each;
-  const int wanted = several ? 4 : !neighbours ? 1 : c->head_dim * (int)elem_size(c->dtype) <= 128 ? 4 : 2;
+  const bool several = s.items > c->n_kv_heads, neighbours = c->head_stride < c->token_stride;
+  const int wanted = several ? 4 : !neighbours ? 1 : c->head_dim * es <= 128 ? 4 : 2;
   s.wave_heads = s.items % wanted == 0 ? wanted : s.items % 2 == 0 && wanted > 1 ? 2 : 1;
-  s.least = LEAST_PER_WAVE * WAVES / s.wave_heads;
-  const int64_t resident = 256 * resident_workgroups(c->head_dim, (int)elem_size(c->dtype)) / (s.items / s.wave_heads);
-  const int64_t most = (c->n_seqs * (tiles > 0 ? tiles : 1) + s.least - 1) / s.least;
-  s.parts = (int)(most < resident ? most : resident);
-  if (s.parts < 1) s.parts = 1;
-  if (s.one_each) s.parts = c->n_seqs;
-  s.nt = (double)c->n_pages * c->page_size * c->n_kv_heads * c->head_dim * 2 * elem_size(c->dtype) > (double)(300 << 20);
+  s.least = LEAST_PER_WAVE * WAVES;
+  const int64_t capacity = (int64_t)c->table_width * c->page_size, tiles = (capacity + tile - 1) / tile;
+  const int64_t resident = 256 * resident_workgroups(c->head_dim, es), pieces = (tiles + s.least - 1) / s.least;
+  // one round of workgroups, and at least one for every item; no more than there can be pieces of work
+  int64_t grid = (int64_t)c->n_seqs * s.items * (pieces > 1 ? pieces : 1);
+  if (grid > resident) grid = resident;
+  if (grid < s.items) grid = s.items;
+  s.grid = (int)grid;
+  s.parts = (int)(grid * (s.items % 4 == 0 ? 4 : s.items % 2 == 0 ? 2 : 1) / s.items);  // the most there can be
+  // sequences that no deal splits
+  const int64_t kept = window > 0 && window + tile < capacity ? window + tile : capacity;
+  s.join = kept > ((int64_t)c->n_seqs * s.items <= grid ? SMALL_PLACES : TINY_PLACES);
+  s.nt = (double)c->n_pages * c->page_size * c->n_kv_heads * c->head_dim * 2 * es > (double)(300 << 20);
   s.ml = align_up((size_t)c->n_seqs * sizeof(int2), 256);
-  const size_t slots = s.one_each ? 0 : (size_t)s.parts * 2;
-  s.o = s.ml + align_up(slots * s.items * s.rows * sizeof(f32x2), 256);
-  s.total = s.o + align_up(slots * s.items * s.rows * c->head_dim * sizeof(float), 256);
-  if (s.total < 256) s.total = 256;
+  s.o = s.ml + align_up((size_t)s.parts * 2 * s.items * s.rows * sizeof(f32x2), 256);
+  s.total = s.o + align_up((size_t)s.parts * 2 * s.items * s.rows * c->head_dim * sizeof(float), 256);
   return s;
 }
 
@@ -569,12 +601,12 @@ void launch(const DecodeArgs& a, unsigned grid, bool nt, hipStream_t s) {
 
 template <typename X>
 int32_t launch_decode(const DecodeArgs& a, const Split& sp, hipStream_t s) {
-  const unsigned grid = (unsigned)((int64_t)sp.parts * (sp.items / sp.wave_heads));
+  const unsigned grid = (unsigned)sp.grid;
   if (a.D <= 64) launch<X, 64>(a, grid, sp.nt, s);
   else if (a.D <= 128) launch<X, 128>(a, grid, sp.nt, s);
   else launch<X, 256>(a, grid, sp.nt, s);
   int32_t st = check_hip(hipGetLastError(), "attention launch");
-  if (st != MOE_OK || sp.one_each) return st;
+  if (st != MOE_OK || !sp.join) return st;
   const int64_t rows = (int64_t)a.n_seqs * a.hq;
   // (a row has about parts / sequences pieces; the weights of four rows' take LDS)
   if (rows >= MANY_ROWS) {
@@ -597,7 +629,7 @@ extern "C" size_t moe_attention_decode_workspace_bytes(const moe_kv_cache* c, in
     fail(MOE_ERR_INVALID_ARG, "n_q_heads=%d must be a multiple of n_kv_heads=%d in 1..%d", n_q_heads, c->n_kv_heads, MOE_MAX_HEADS);
     return 0;
   }
-  return split_of(c, n_q_heads).total;
+  return split_of(c, n_q_heads, 0).total;
 }
 
 extern "C" int32_t moe_attention_decode(const moe_kv_cache* c, int32_t n_q_heads, const moe_head_rows* q, const int32_t* seq_lens,
@@ -616,7 +648,7 @@ extern "C" int32_t moe_attention_decode(const moe_kv_cache* c, int32_t n_q_heads
   const int64_t es = (int64_t)elem_size(c->dtype);
   if (!rows_aligned(q, es) || !rows_aligned(out, es))
     return fail(MOE_ERR_INVALID_ARG, "moe_attention_decode: pointers and strides of q and out must be multiples of 16 bytes");
-  const Split sp = split_of(c, n_q_heads);
+  const Split sp = split_of(c, n_q_heads, opt->window);
   if ((int64_t)c->n_seqs * n_q_heads > INT32_MAX)
     return fail(MOE_ERR_UNSUPPORTED, "moe_attention_decode: %d sequences of %d query heads are too many for one call", c->n_seqs, n_q_heads);
   if (!ws || ((uintptr_t)ws & 255) || ws_bytes < need)
@@ -656,8 +688,7 @@ extern "C" int32_t moe_attention_decode(const moe_kv_cache* c, int32_t n_q_heads
   a.window = opt->window;
   a.least = sp.least;
   a.parts = sp.parts;
-  a.one_each = sp.one_each;
-  a.inverse_parts = 1.0 / sp.parts;
+  a.may_split = sp.join;
   a.scale = opt->scale;
   a.cap = opt->softcap;
   a.inv_cap = opt->softcap > 0.f ? 1.f / opt->softcap : 0.f;
