@@ -576,9 +576,15 @@ Split split_of(const moe_kv_cache* c, int32_t n_q_heads, int32_t window) {
   if (grid < s.items) grid = s.items;
   s.grid = (int)grid;
   s.parts = (int)(grid * (s.items % 4 == 0 ? 4 : s.items % 2 == 0 ? 2 : 1) / s.items);  // the most there can be
-  // sequences that no deal splits
+  // sequences that no deal splits: no second launch, and no look at all the lengths
   const int64_t kept = window > 0 && window + tile < capacity ? window + tile : capacity;
-  s.join = kept > ((int64_t)c->n_seqs * s.items <= grid ? SMALL_PLACES : TINY_PLACES);
+  const int64_t work = (int64_t)c->n_seqs * s.items;
+  s.join = kept > SMALL_PLACES;
+  if (!s.join && work > grid) {
+    // more short sequences than one round holds: a workgroup for each, so that the long ones among them do not meet
+    const int wave_heads = kept > TINY_PLACES ? s.wave_heads : s.items % 4 == 0 ? 4 : s.items % 2 == 0 ? 2 : 1;
+    s.grid = (int)(work / wave_heads);
+  }
   s.nt = (double)c->n_pages * c->page_size * c->n_kv_heads * c->head_dim * 2 * es > (double)(300 << 20);
   s.ml = align_up((size_t)c->n_seqs * sizeof(int2), 256);
   s.o = s.ml + align_up((size_t)s.parts * 2 * s.items * s.rows * sizeof(f32x2), 256);

@@ -57,6 +57,21 @@ def test_many_sequences():
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,D", [(8, 8, 64), (6, 6, 64), (5, 5, 64), (4, 1, 128), (48, 4, 64), (80, 2, 64), (8, 4, 256)])
+def test_deals(hq, hkv, D, dtype):
+    """The ways the work is dealt out: tables far wider than the lengths, all sequences short, some long, more sequences than
+    workgroups, heads side by side or not."""
+    rng = np.random.default_rng(hq)
+    wide = dict(spare_width=300)
+    run(rng.integers(0, 100, 200).tolist(), hq, hkv, D, 16, dtype, **wide)                      # all tiny
+    run(rng.integers(0, 100, 200).tolist(), hq, hkv, D, 16, dtype, "head_major", window=3)
+    run(rng.integers(0, 900, 12).tolist(), hq, hkv, D, 16, dtype, **wide)                       # short, fewer than workgroups
+    run(rng.integers(0, 300, 150).tolist(), hq, hkv, D, 16, dtype)                              # short by the table, more than workgroups
+    run(rng.integers(0, 300, 150).tolist(), hq, hkv, D, 16, dtype, **wide)                      # short, found out from the lengths
+    run([2000] + rng.integers(0, 40, 80).tolist() + [1500], hq, hkv, D, 16, dtype, "head_major")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("window", [1, 2, 16, 100, 129, 100000])
 def test_window(window, dtype):
     run(RAGGED + [1000], 4, 2, 64, 16, dtype, window=window)
