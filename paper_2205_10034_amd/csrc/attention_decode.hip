@@ -52,8 +52,13 @@ struct DecodeArgs {
   f32x2* part_ml;  // [slot][items][rows]
   int2* plan;      // [sequence]: slot of the first piece, pieces
   int64_t n_pages, page_stride, token_stride, head_stride, q_token, q_head, o_token, o_head;  // bytes
-  PageDivisor page;
-  int32_t page_size, table_width, n_seqs, hq, hkv, G, rows, items, hts, wave_heads, parts, may_split, D, window, least;
+  PageDivisor page, per_kv_head, per_rows;  // places of a page, items of a kv head, rows of an item
+  struct {
+    PageDivisor per_part;  // workgroups of a part
+    int32_t parts;
+    double inverse_parts;
+  } share_of_grid[3];  // with 1, 2 and 4 items a workgroup
+  int32_t page_size, table_width, capacity, n_seqs, hq, hkv, G, rows, items, hts, log_heads, parts, may_split, D, window, least;
   float scale, cap, inv_cap;
 };
 
@@ -69,9 +74,10 @@ template <int BYTES> struct Words;
 template <> struct Words<8> { typedef u32x2 type; };
 template <> struct Words<16> { typedef u32x4 type; };
 
-// How many of the neighbouring items one workgroup takes so that the `rows` fit `grid` workgroups, if they can.
+// How many of the neighbouring items, 2 to the power of what comes back, one workgroup takes so that the `rows` fit `grid`
+// workgroups, if they can.
 __device__ __forceinline__ int side_by_side(int items, int64_t rows, int64_t grid) {
-  return rows <= grid || items % 2 ? 1 : rows <= 2 * grid || items % 4 ? 2 : 4;
+  return rows <= grid || items % 2 ? 0 : rows <= 2 * grid || items % 4 ? 1 : 2;
 }
 
 // A value that all lanes hold, for the scalar registers.
@@ -82,40 +88,42 @@ __device__ __forceinline__ int64_t uniform(int64_t v, int lane) {
 
 // How the workgroups share the batch, from its lengths: a wavefront's place in it.  Every wavefront finds it by itself.
 struct Deal {
-  int wave_heads, groups, w;  // items of a workgroup, workgroups that share a part, the part
+  int log_heads, first_item, w;  // items of a workgroup (their logarithm), the first of them, the part
   bool one_each;              // the row counts sequences, not tiles: no sequence is split
   int64_t share, total;       // of a part, of the row
   int64_t begin;              // where in the row sequence b begins
-  int b, n;                   // the part's first sequence, its kept length
+  int b, len;                 // the part's first sequence, its length
 };
-__device__ __forceinline__ int length_of(const DecodeArgs& a, int b) { return kept_length(a.lens[b], a.table_width * a.page_size); }
 
 __device__ __forceinline__ Deal deal(const DecodeArgs& a, int tile) {
   const int lane = threadIdx.x & 63, id = blockIdx.x;
-  auto tiles_in = [&](int n) { return kept_tiles(n, first_place(n, a.window), tile); };
+  auto tiles_in = [&](int len) {
+    const int n = kept_length(len, a.capacity);
+    return kept_tiles(n, first_place(n, a.window), tile);
+  };
   const int64_t rows = (int64_t)a.n_seqs * a.items, grid = gridDim.x;
   Deal p{};
-  auto take = [&](int wave_heads) {
-    p.wave_heads = wave_heads;
-    p.groups = a.items / wave_heads;
-    p.w = id / p.groups;
-    return (int)grid / p.groups;  // parts
+  auto take = [&](int log_heads) {
+    p.log_heads = log_heads;
+    p.w = a.share_of_grid[log_heads].per_part.quotient(id);
+    p.first_item = (id - p.w * (a.items >> log_heads)) << log_heads;
   };
   auto whole = [&] {
-    const int parts = take(side_by_side(a.items, rows, grid));
+    take(side_by_side(a.items, rows, grid));
+    const auto& g = a.share_of_grid[p.log_heads];
     p.one_each = true;
-    p.share = (a.n_seqs + parts - 1) / parts;
+    p.share = (int64_t)(((double)(a.n_seqs + g.parts) - 0.5) * g.inverse_parts);  // rounded up: half a unit from where the product's rounding could matter
     p.total = a.n_seqs;
     p.begin = p.w * p.share;
     p.b = (int)p.begin;
-    if (p.begin < p.total) p.n = length_of(a, p.b);
+    if (p.begin < p.total) p.len = a.lens[p.b];
     return p;
   };
   if (!a.may_split) return whole();
-  int n = lane < a.n_seqs ? length_of(a, lane) : 0, longest = tiles_in(n);
+  int len = lane < a.n_seqs ? a.lens[lane] : 0, longest = tiles_in(len);
   int64_t mine = lane < a.n_seqs ? row_tiles(longest) : 0, total = mine;
   for (int s = lane + 64; s < a.n_seqs; s += 64) {
-    const int t = tiles_in(length_of(a, s));
+    const int t = tiles_in(a.lens[s]);
     longest = t > longest ? t : longest;
     total += row_tiles(t);
   }
@@ -123,8 +131,8 @@ __device__ __forceinline__ Deal deal(const DecodeArgs& a, int tile) {
   if (tiny || (small && rows <= grid)) return whole();
   for (int d = 1; d < 64 && d < a.n_seqs; d <<= 1) total += __shfl_xor(total, d, 64);
   p.total = uniform(total, 0);
-  const int parts = take(p.total * tile < (int64_t)a.n_seqs * SMALL_PLACES && rows >= 2 * grid ? side_by_side(a.items, rows, grid) : a.wave_heads);
-  p.share = uniform(share_of_row(p.total, 1.0 / parts, a.least / p.wave_heads), 0);
+  take(p.total * tile < (int64_t)a.n_seqs * SMALL_PLACES && rows >= 2 * grid ? side_by_side(a.items, rows, grid) : a.log_heads);
+  p.share = uniform(share_of_row(p.total, a.share_of_grid[p.log_heads].inverse_parts, a.least >> p.log_heads), 0);
   const int64_t at = p.w * p.share;
   if (at >= p.total) return p;
   for (int s = 0;;) {
@@ -137,14 +145,14 @@ __device__ __forceinline__ Deal deal(const DecodeArgs& a, int tile) {
     if (beyond) {
       const int who = __ffsll(beyond) - 1;
       p.b = s + who;
-      p.n = __builtin_amdgcn_readlane(n, who);
+      p.len = __builtin_amdgcn_readlane(len, who);
       p.begin += uniform(upto - mine, who);
       return p;
     }
     p.begin += uniform(upto, 63);
     s += 64;
-    n = s + lane < a.n_seqs ? length_of(a, s + lane) : 0;
-    mine = s + lane < a.n_seqs ? row_tiles(tiles_in(n)) : 0;
+    len = s + lane < a.n_seqs ? a.lens[s + lane] : 0;
+    mine = s + lane < a.n_seqs ? row_tiles(tiles_in(len)) : 0;
   }
 }
 
@@ -216,11 +224,11 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) voi
   const int m16 = lane & 15, g = lane >> 4, piece = (g + 4 * (m16 >> 3)) * 16;
   // wavefronts of a workgroup: wave_heads neighbouring items, `step` of them on the tiles of each in turn
   Deal at = deal(a, TILE);
-  const int wave_heads = at.wave_heads, w = at.w, step = WAVES / wave_heads;
+  const int wave_heads = 1 << at.log_heads, w = at.w, step = WAVES >> at.log_heads;
   int64_t x = w * at.share;
   const int64_t x_end = x + at.share < at.total ? x + at.share : at.total;
   if (x >= x_end) return;
-  const int item = blockIdx.x % at.groups * wave_heads + wave % wave_heads, hk = item / a.hts, ht = item % a.hts;
+  const int item = at.first_item + (wave & (wave_heads - 1)), hk = a.per_kv_head.quotient(item), ht = item - hk * a.hts;
   auto heads_of = [&](int tile_of_heads) { return a.G - tile_of_heads * HEADS < HEADS ? a.G - tile_of_heads * HEADS : HEADS; };
   const int my_heads = heads_of(ht);
   const char* zeros = reinterpret_cast<const char*>(ZEROS);
@@ -233,16 +241,28 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) voi
   for (int piece_no = 0; x < x_end; ++piece_no) {
   // the piece of sequence b that lies in this part
   const int b = at.b;
-  const int n = at.n, first = first_place(n, a.window), tile0 = first / TILE, tiles = kept_tiles(n, first, TILE);
+  const int32_t* table = a.table + (int64_t)b * a.table_width;
+  // the table's entry for this lane's place of tile tt; an entry of the table in any case
+  auto entry_of = [&](int tt) {
+    const unsigned column = (unsigned)a.page.quotient((int)((unsigned)tt * TILE + tp)), last = (unsigned)a.table_width - 1u;
+    return table[column < last ? column : last];
+  };
+  const int from = (int)(x - at.begin), mine = from + (wave >> at.log_heads);
+  // without a window the first tiles are known before the length is
+  const bool early = a.window == 0 && a.table_width > 0;
+  int now = -1, entry = -1;
+  if (early) {
+    now = entry_of(mine);
+    entry = entry_of(mine + step);
+  }
+  const int n = kept_length(at.len, a.capacity), first = first_place(n, a.window), tile0 = first / TILE, tiles = kept_tiles(n, first, TILE);
   const int64_t b_end = at.begin + (at.one_each ? 1 : row_tiles(tiles));
-  const int from = (int)(x - at.begin), upto = b_end <= x_end ? tiles : (int)(x_end - at.begin);
+  const int upto = b_end <= x_end ? tiles : (int)(x_end - at.begin);
   const bool whole = from == 0 && b_end <= x_end;
   const int slot = 2 * w + (piece_no > 0);
-  if (from == 0 && threadIdx.x == 0 && item == 0)
-    a.plan[b] = make_int2(slot, whole ? 1 : (int)((b_end - 1) / at.share) - w + 1);
+  if (from == 0 && threadIdx.x == 0 && item == 0) a.plan[b] = make_int2(slot, whole ? 1 : part_of(b_end - 1, at.share) - w + 1);
   const int t_end = tiles ? tile0 + upto : 0;
-  int t = tile0 + from + wave / wave_heads;
-  const int32_t* table = a.table + (int64_t)b * a.table_width;
+  int t = tile0 + mine;
 
   // Nothing in the loop that loads is conditional: what a tile beyond the last one would load is ZEROS.  (Behind a branch the
   // compiler waits for every load in flight before it uses the first.)
@@ -250,8 +270,6 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) voi
     const int p = (int)((unsigned)tt * TILE + tp);
     return tt < t_end && p >= first && p < n;
   };
-  // the table's entry for this lane's place of tile tt
-  auto entry_of = [&](int tt) { return table[is_kept(tt) ? a.page.quotient((int)((unsigned)tt * TILE + tp)) : 0]; };
   // rows of tile tt into LDS; returns which places are kept
   auto place_rows = [&](int tt, int entry) {
     const int p = (int)((unsigned)tt * TILE + tp), page = is_kept(tt) ? valid_page(entry, a.n_pages) : -1;
@@ -306,8 +324,10 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) voi
     const char* q_row = a.q + (int64_t)b * a.q_token + (int64_t)(hk * a.G + ht * HEADS + m16) * a.q_head + g * 16;
 #pragma unroll
     for (int s = 0; s < KSTEPS; ++s) qr[s] = read<false, u32x4>(have && (s * 64 + g * 16) < a.D * (int)sizeof(X) ? q_row + s * 64 : zeros);
-    const int now = entry_of(t);
-    int entry = entry_of(t + step);
+    if (!early) {
+      now = entry_of(t);
+      entry = entry_of(t + step);
+    }
     uint32_t kept = place_rows(t, now);
     __builtin_amdgcn_sched_barrier(0);  // (the loop counts on the keys being requested first)
     load_keys();
@@ -431,7 +451,7 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) voi
   // (wavefront w and those a multiple of wave_heads away have the same kv head)
   auto joined_max = [&](int w, int row) {
     float top = -INFINITY;
-    for (w %= wave_heads; w < WAVES; w += wave_heads) top = fmaxf(top, ml_lds[w][row][0]);
+    for (w &= wave_heads - 1; w < WAVES; w += wave_heads) top = fmaxf(top, ml_lds[w][row][0]);
     return top;
   };
   auto part_weight = [&](int w, int row, float top) { return top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml_lds[w][row][0] - top); };
@@ -452,8 +472,9 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) voi
     lds_barrier();
     const int dim = blk * BD + d;
     for (int i = threadIdx.x / (BD / 4); i < a.rows * wave_heads; i += 64 * WAVES / (BD / 4)) {
-      const int wh = i / a.rows, r = i % a.rows, its = item - wave % wave_heads + wh;  // the row's item
-      if (r >= heads_of(its % a.hts)) continue;
+      const int wh = a.per_rows.quotient(i), r = i - wh * a.rows, its = at.first_item + wh;  // the row's item
+      const int its_hk = a.per_kv_head.quotient(its), its_ht = its - its_hk * a.hts;
+      if (r >= heads_of(its_ht)) continue;
       const float top = joined_max(wh, r);
       float sum = 0.f;
       f32x4 y{0.f, 0.f, 0.f, 0.f};
@@ -463,7 +484,7 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) voi
       }
       if (!FULL && dim >= a.D) continue;
       if (whole) {
-        store_row<X>(a, b, its / a.hts * a.G + its % a.hts * HEADS + r, dim, y, sum, top);
+        store_row<X>(a, b, its_hk * a.G + its_ht * HEADS + r, dim, y, sum, top);
       } else {
         const int64_t part = ((int64_t)slot * a.items + its) * a.rows + r;
         *reinterpret_cast<f32x4*>(a.part_o + part * a.D + dim) = y;
@@ -473,7 +494,7 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) voi
   }
   x = b_end;
   at.begin = b_end;
-  if (x < x_end) at.n = length_of(a, ++at.b);
+  if (x < x_end) at.len = a.lens[++at.b];
   }
 }
 
@@ -688,8 +709,18 @@ extern "C" int32_t moe_attention_decode(const moe_kv_cache* c, int32_t n_q_heads
   a.G = n_q_heads / c->n_kv_heads;
   a.rows = sp.rows;
   a.items = sp.items;
-  a.wave_heads = sp.wave_heads;
+  a.log_heads = sp.wave_heads >> 1;
+  for (int k = 0; k < 3; ++k) {
+    const int groups = sp.items >> k;
+    if (groups == 0) continue;  // (never taken)
+    a.share_of_grid[k].per_part = page_divisor(groups);
+    a.share_of_grid[k].parts = sp.grid / groups;
+    a.share_of_grid[k].inverse_parts = 1.0 / a.share_of_grid[k].parts;
+  }
   a.hts = sp.items / c->n_kv_heads;
+  a.per_kv_head = page_divisor(a.hts);
+  a.per_rows = page_divisor(sp.rows);
+  a.capacity = c->table_width * c->page_size;
   a.D = c->head_dim;
   a.window = opt->window;
   a.least = sp.least;

@@ -44,6 +44,13 @@ MOESYS_HD int64_t share_of_row(int64_t total, double inverse, int least) {
   const int64_t share = (int64_t)((double)total * inverse) + 1;
   return share < least ? least : share;
 }
+// Part that tile `at` of the row lies in; the quotient in float64 is off by one at most.
+MOESYS_HD int part_of(int64_t at, int64_t share) {
+  int64_t w = (int64_t)((double)at / (double)share);
+  if (w * share > at) --w;
+  if ((w + 1) * share <= at) ++w;
+  return (int)w;
+}
 // Pieces that can be unfinished are a part's first and its last: two slots for each part, 2w for the first piece.  Slot of piece j of
 // a sequence whose first piece has slot `first`: it goes on as the first piece of the parts that follow.
 MOESYS_HD int piece_slot(int first, int j) { return j == 0 ? first : (first / 2 + j) * 2; }

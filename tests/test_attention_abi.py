@@ -225,7 +225,8 @@ int main() {
         const int slot = 2 * w + (no > 0);
         if (x == begin) {
           first[b] = slot;
-          const int expected = whole ? 1 : (int)((b_end - 1) / share) - w + 1;
+          assert(part_of(b_end - 1, share) == (int)((b_end - 1) / share));
+          const int expected = whole ? 1 : part_of(b_end - 1, share) - w + 1;
           pieces[b] = -expected;
         }
         if (!whole) { assert(used[slot] < 0); used[slot] = b; }
@@ -237,6 +238,13 @@ int main() {
       }
     }
     assert(covered == total);
+  }
+  for (int i = 0; i < 200000; ++i) {
+    const long long share = 1 + next() % (i % 2 ? 50 : 1 << 24), part = next() % 2000;
+    for (int e = -1; e < 2; ++e) if (part * share + e >= 0) assert(part_of(part * share + e, share) == (part * share + e) / share);
+    // sequences of a part, as the kernel rounds them up
+    const int S = 1 + next() % (i % 3 ? 600 : 1 << 30), parts = 1 + next() % (i % 5 ? 2048 : 1 << 20);
+    assert((long long)(((double)(S + parts) - 0.5) * (1.0 / parts)) == ((long long)S + parts - 1) / parts);
   }
   // the quotient in float64, at its worst
   for (long long total : {1ll, 2ll, 3ll, 1000000007ll, (1ll << 40) - 1, 1ll << 40, (1ll << 40) + 1})
