@@ -1,19 +1,28 @@
 // Attention of one new token per sequence over a paged cache (moe_attention_decode): one pass over the keys and values
 // with the running maximum m and sum l of the softmax,
 //   m' = max(m, z_j);  l' = l exp(m - m') + exp(z_j - m');  o' = o exp(m - m') + exp(z_j - m') v_j;  out = o / l,
-// split over the length into chunks whose (m, l, o) are joined at the end with the weights exp(m_i - max m).
+// split over the length into pieces whose (m, l, o) are joined at the end with the weights exp(m_i - max m).
 //
-// Bound: HBM, every key and value once; the arithmetic is G = query heads per kv head multiply-adds per element.  So
-// the kernel is built around loads that go from memory into the registers that the matrix instructions read:
-//  - A wavefront takes tiles of 32 (bfloat16) or 16 (float32) places and the up to 16 query heads of one kv head.
-//  - Scores: S^T[place, head] = K Q^T, keys as the first operand: a lane loads 16 bytes of one key.  The contraction index
-//    of an instruction may be any permutation of the dimensions as long as both operands use it.
-//  - Output: O^T[dim, head] += V^T P^T.  A lane of S^T holds four places of one head, which is how the second operand wants
-//    P^T when the places of an instruction are taken in that order: no data moves between lanes.  The first operand has to
-//    hold eight places of one dimension: a lane loads the same EPL dimensions of those eight places and pairs the halves
-//    with one v_perm per four bytes, row m of the instruction standing for dimension m*EPL + j in the j-th of EPL products.
-//  - Keys of the next tile are requested when this tile's scores are formed, values when its output is: two kinds of
-//    loads of a tile are in flight while the other kind is used, and the wavefronts of the CU hide the rest.
+// Bound: HBM, every key and value once; the arithmetic is G = query heads per kv head multiply-adds per element.  So the kernel
+// is built around loads that go from memory into the registers that the matrix instructions read:
+//  - A wavefront takes tiles of 32 places (16 in float32, and beyond 128 dimensions, where registers are short) and the up to 16
+//    query heads of one kv head.
+//  - Scores: S^T[place, head] = K Q^T, keys as the first operand.  The contraction index of an instruction may be any permutation
+//    of the dimensions as long as both operands use it.  A load brings eight keys' whole 128-byte lines: rows 0-7 of the operand
+//    are those keys' first half lines and rows 8-15 their second ones, so each operand is multiplied with both halves of the
+//    queries and half of each product is used.  (16 half lines per load, which need no second product, read 1.3 GB in 250 us;
+//    whole ones in 232, and only they gain from loads past the caches.)
+//  - Output: O^T[dim, head] += V^T P^T.  A lane of S^T holds four places of one head, which is how the second operand wants P^T
+//    when the places of an instruction are taken in that order: no data moves between lanes.  The first operand has to hold eight
+//    places of one dimension: a lane loads the same EPL dimensions of those places and pairs the halves with one v_perm per four
+//    bytes, row m of the instruction standing for dimension m*EPL + j in the j-th of EPL products.
+//  - Keys of the next tile are requested when this tile's scores are formed, values when its output is: one kind of loads is in
+//    flight while the other is used, and the other wavefronts of the CU hide the rest.
+//  - All sequences' tiles stand in one row that the resident workgroups share evenly (Deal): no last round, no long sequence that
+//    the others wait for.
+// Measured: 256 sequences of 2048 to 14336 places, 64 query and 8 kv heads of 128 (8.5 GB of keys and values) 1253 us, 6.8 TB/s; 64 of
+// 100 to 8192 (1.3 GB) 200 us, 6.5 TB/s; one of 131071 (0.54 GB) 89 us, of which the join takes 5; one of 173, 16 heads of 64: 7 us,
+// four dependent trips to memory.
 #include "attention_internal.h"
 #include "wave_util.h"
 
@@ -30,7 +39,17 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int WAVES = 4;
 constexpr int HEADS = 16;  // query heads of a tile
-constexpr int LEAST_PER_WAVE = 2, MANY_ROWS = 1024, TINY_PLACES = 128, SMALL_PLACES = 1024;
+// Tiles of a part for each of its wavefronts, at least: 8 sequences of 100 to 1500 places take 17.2 us with 2, 18.4 with 1 and 19.4
+// with 4 (more pieces to join, fewer CUs at work).
+constexpr int LEAST_PER_WAVE = 2;
+// Joins of so many rows take a wavefront each: 16384 rows of 2 to 3 pieces 6.5 us, 12.2 with a workgroup each.
+constexpr int MANY_ROWS = 1024;
+// Sequences that are not split.  None longer than TINY_PLACES: a piece's four trips to memory are all there is, so the fewest rounds
+// of workgroups count (292 sequences of one place, 16 heads of 192: 24 us; shared evenly, 9 pieces one after the other per
+// workgroup, 68).  None longer than SMALL_PLACES, and a workgroup for each: the join would cost more than it saves (one of 173
+// places 7 us and 12, 16 of up to 1000 places 15.4 and 18.1, 512 of up to 700 131 and 140; 256 of up to 2000 are better shared,
+// 171 against 186).
+constexpr int TINY_PLACES = 128, SMALL_PLACES = 1024;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 // Rows of places that are not there and dimensions beyond head_dim are read from here: no load leaves the caller's rows, and what
@@ -221,7 +240,7 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) voi
   __shared__ f32x2 ml_lds[WAVES][HEADS];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int m16 = lane & 15, g = lane >> 4, piece = (g + 4 * (m16 >> 3)) * 16;
+  const int m16 = lane & 15, g = lane >> 4, line_at = (g + 4 * (m16 >> 3)) * 16;
   // wavefronts of a workgroup: wave_heads neighbouring items, `step` of them on the tiles of each in turn
   Deal at = deal(a, TILE);
   const int wave_heads = 1 << at.log_heads, w = at.w, step = WAVES >> at.log_heads;
@@ -239,262 +258,262 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) voi
   const float slope = a.slopes && m16 < my_heads ? a.slopes[hk * a.G + ht * HEADS + m16] : 0.f;
 
   for (int piece_no = 0; x < x_end; ++piece_no) {
-  // the piece of sequence b that lies in this part
-  const int b = at.b;
-  const int32_t* table = a.table + (int64_t)b * a.table_width;
-  // the table's entry for this lane's place of tile tt; an entry of the table in any case
-  auto entry_of = [&](int tt) {
-    const unsigned column = (unsigned)a.page.quotient((int)((unsigned)tt * TILE + tp)), last = (unsigned)a.table_width - 1u;
-    return table[column < last ? column : last];
-  };
-  const int from = (int)(x - at.begin), mine = from + (wave >> at.log_heads);
-  // without a window the first tiles are known before the length is
-  const bool early = a.window == 0 && a.table_width > 0;
-  int now = -1, entry = -1;
-  if (early) {
-    now = entry_of(mine);
-    entry = entry_of(mine + step);
-  }
-  const int n = kept_length(at.len, a.capacity), first = first_place(n, a.window), tile0 = first / TILE, tiles = kept_tiles(n, first, TILE);
-  const int64_t b_end = at.begin + (at.one_each ? 1 : row_tiles(tiles));
-  const int upto = b_end <= x_end ? tiles : (int)(x_end - at.begin);
-  const bool whole = from == 0 && b_end <= x_end;
-  const int slot = 2 * w + (piece_no > 0);
-  if (from == 0 && threadIdx.x == 0 && item == 0) a.plan[b] = make_int2(slot, whole ? 1 : part_of(b_end - 1, at.share) - w + 1);
-  const int t_end = tiles ? tile0 + upto : 0;
-  int t = tile0 + mine;
-
-  // Nothing in the loop that loads is conditional: what a tile beyond the last one would load is ZEROS.  (Behind a branch the
-  // compiler waits for every load in flight before it uses the first.)
-  auto is_kept = [&](int tt) {
-    const int p = (int)((unsigned)tt * TILE + tp);
-    return tt < t_end && p >= first && p < n;
-  };
-  // rows of tile tt into LDS; returns which places are kept
-  auto place_rows = [&](int tt, int entry) {
-    const int p = (int)((unsigned)tt * TILE + tp), page = is_kept(tt) ? valid_page(entry, a.n_pages) : -1;
-    const int in_page = p - a.page.quotient(p) * a.page_size;
-    const char* row = page >= 0 ? base + page * a.page_stride + in_page * a.token_stride : zeros;
-    if (TILE == 32 || (lane & 16) == 0) row_at[wave][lane >> 5][tp] = reinterpret_cast<uint64_t>(row);
-    const uint32_t kept = (uint32_t)__ballot(page >= 0) & EVERY;
-    asm volatile("" ::: "memory");  // (a wavefront's LDS operations execute in order)
-    return kept;
-  };
-
-  u32x4 kr[SUB][2][LINES];
-  VWord vr[NV][NBLK];
-  // 8 keys' whole 128-byte lines per instruction: lane (m16, g) has piece g + 4 (m16 / 8) of key m16 % 8
-  auto load_keys = [&]() {
-#pragma unroll
-    for (int st = 0; st < SUB; ++st)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const char* row = reinterpret_cast<const char*>(row_at[wave][0][st * 16 + e * 8 + (m16 & 7)]) + piece;
-#pragma unroll
-        for (int c = 0; c < LINES; ++c) {
-          const char* p = row + c * 128;
-          if (!FULL && c * 128 + piece >= a.D * (int)sizeof(X)) p = zeros;
-          kr[st][e][c] = read<NT, u32x4>(p);
-        }
-      }
-  };
-  auto load_values = [&]() {
-#pragma unroll
-    for (int u = 0; u < NV; ++u) {
-      const char* row = reinterpret_cast<const char*>(row_at[wave][1][u / 4 * 16 + g * 4 + u % 4]) + m16 * (EPL * sizeof(X));
-#pragma unroll
-      for (int blk = 0; blk < NBLK; ++blk) {
-        const char* p = row + blk * (BD * sizeof(X));
-        if (!FULL && (blk * 16 + m16) * EPL >= a.D) p = zeros;
-        vr[u][blk] = read<NT, VWord>(p);
-      }
+    // the piece of sequence b that lies in this part
+    const int b = at.b;
+    const int32_t* table = a.table + (int64_t)b * a.table_width;
+    // the table's entry for this lane's place of tile tt; an entry of the table in any case
+    auto entry_of = [&](int tt) {
+      const unsigned column = (unsigned)a.page.quotient((int)((unsigned)tt * TILE + tp)), last = (unsigned)a.table_width - 1u;
+      return table[column < last ? column : last];
+    };
+    const int from = (int)(x - at.begin), mine = from + (wave >> at.log_heads);
+    // without a window the first tiles are known before the length is
+    const bool early = a.window == 0 && a.table_width > 0;
+    int now = -1, entry = -1;
+    if (early) {
+      now = entry_of(mine);
+      entry = entry_of(mine + step);
     }
-  };
+    const int n = kept_length(at.len, a.capacity), first = first_place(n, a.window), tile0 = first / TILE, tiles = kept_tiles(n, first, TILE);
+    const int64_t b_end = at.begin + (at.one_each ? 1 : row_tiles(tiles));
+    const int upto = b_end <= x_end ? tiles : (int)(x_end - at.begin);
+    const bool whole = from == 0 && b_end <= x_end;
+    const int slot = 2 * w + (piece_no > 0);
+    if (from == 0 && threadIdx.x == 0 && item == 0) a.plan[b] = make_int2(slot, whole ? 1 : part_of(b_end - 1, at.share) - w + 1);
+    const int t_end = tiles ? tile0 + upto : 0;
+    int t = tile0 + mine;
 
-  float m = -INFINITY, mref = 0.f, l = 0.f;
-  f32x4 o[NBLK][EPL];
-#pragma unroll
-  for (int blk = 0; blk < NBLK; ++blk)
-#pragma unroll
-    for (int j = 0; j < EPL; ++j) o[blk][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // Nothing in the loop that loads is conditional: what a tile beyond the last one would load is ZEROS.  (Behind a branch the
+    // compiler waits for every load in flight before it uses the first.)
+    auto is_kept = [&](int tt) {
+      const int p = (int)((unsigned)tt * TILE + tp);
+      return tt < t_end && p >= first && p < n;
+    };
+    // rows of tile tt into LDS; returns which places are kept
+    auto place_rows = [&](int tt, int entry) {
+      const int p = (int)((unsigned)tt * TILE + tp), page = is_kept(tt) ? valid_page(entry, a.n_pages) : -1;
+      const int in_page = p - a.page.quotient(p) * a.page_size;
+      const char* row = page >= 0 ? base + page * a.page_stride + in_page * a.token_stride : zeros;
+      if (TILE == 32 || (lane & 16) == 0) row_at[wave][lane >> 5][tp] = reinterpret_cast<uint64_t>(row);
+      const uint32_t kept = (uint32_t)__ballot(page >= 0) & EVERY;
+      asm volatile("" ::: "memory");  // (a wavefront's LDS operations execute in order)
+      return kept;
+    };
 
-  if (t < t_end) {
-    u32x4 qr[KSTEPS];
-    const bool have = m16 < my_heads;
-    const char* q_row = a.q + (int64_t)b * a.q_token + (int64_t)(hk * a.G + ht * HEADS + m16) * a.q_head + g * 16;
-#pragma unroll
-    for (int s = 0; s < KSTEPS; ++s) qr[s] = read<false, u32x4>(have && (s * 64 + g * 16) < a.D * (int)sizeof(X) ? q_row + s * 64 : zeros);
-    if (!early) {
-      now = entry_of(t);
-      entry = entry_of(t + step);
-    }
-    uint32_t kept = place_rows(t, now);
-    __builtin_amdgcn_sched_barrier(0);  // (the loop counts on the keys being requested first)
-    load_keys();
-    __builtin_amdgcn_sched_barrier(0);
-    load_values();
-  do {
-    const uint32_t here = kept;
-    const int entry_next = entry_of(t + 2 * step);
-    f32x4 z[SUB];
-#pragma unroll
-    for (int st = 0; st < SUB; ++st) {
-      // [e][h]: keys e*8.. by the pieces 4h..4h+3 of their lines; rows 8h..8h+7 of the product are the ones that mean something
-      f32x4 part[2][2];
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          part[e][h] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int c = 0; c < LINES; ++c) part[e][h] = product<BF16>(kr[st][e][c], qr[2 * c + h], part[e][h]);
-        }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        // a place's other half lies 32 lanes away
-        const float mine = lane < 32 ? part[0][0][i] : part[1][1][i], other = lane < 32 ? part[1][0][i] : part[0][1][i];
-        z[st][i] = mine + other_half(other, lane);
-      }
-    }
-    kept = place_rows(t + step, entry);
-    entry = entry_next;
-    load_keys();
-    // scores in units of log 2
-    if (plain) {
-#pragma unroll
-      for (int st = 0; st < SUB; ++st) z[st] *= scale2;
-    } else {
+    u32x4 kr[SUB][2][LINES];
+    VWord vr[NV][NBLK];
+    // 8 keys' whole 128-byte lines per instruction: lane (m16, g) has piece g + 4 (m16 / 8) of key m16 % 8
+    auto load_keys = [&]() {
 #pragma unroll
       for (int st = 0; st < SUB; ++st)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float s = z[st][i] * a.scale;
-          if (a.cap > 0.f) s = a.cap * tanhf(s * a.inv_cap);
-          s -= slope * (float)(n - 1 - (t * TILE + st * 16 + g * 4 + i));
-          z[st][i] = s * LOG2E;
+        for (int e = 0; e < 2; ++e) {
+          const char* row = reinterpret_cast<const char*>(row_at[wave][0][st * 16 + e * 8 + (m16 & 7)]) + line_at;
+#pragma unroll
+          for (int c = 0; c < LINES; ++c) {
+            const char* p = row + c * 128;
+            if (!FULL && c * 128 + line_at >= a.D * (int)sizeof(X)) p = zeros;
+            kr[st][e][c] = read<NT, u32x4>(p);
+          }
         }
-    }
-    if (here != EVERY) {
+    };
+    auto load_values = [&]() {
 #pragma unroll
-      for (int st = 0; st < SUB; ++st)
+      for (int u = 0; u < NV; ++u) {
+        const char* row = reinterpret_cast<const char*>(row_at[wave][1][u / 4 * 16 + g * 4 + u % 4]) + m16 * (EPL * sizeof(X));
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (!((here >> (st * 16 + g * 4 + i)) & 1)) z[st][i] = -INFINITY;
-    }
-    float top = z[0][0];
-#pragma unroll
-    for (int st = 0; st < SUB; ++st)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) top = fmaxf(top, z[st][i]);
-    // The maximum moves only when some score passes it by a factor of 2^8: until then the weights grow to at most that, which
-    // float32 sums do not mind, and the four lanes of a head need not exchange theirs.
-    if (__any(top > m + 8.f)) {
-      top = fmaxf(top, __shfl_xor(top, 16, 64));
-      top = fmaxf(top, __shfl_xor(top, 32, 64));
-      const float now = fmaxf(m, top), f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - now);
-      m = now;
-      mref = now == -INFINITY ? 0.f : now;
-      l *= f;
-#pragma unroll
-      for (int blk = 0; blk < NBLK; ++blk)
-#pragma unroll
-        for (int j = 0; j < EPL; ++j) o[blk][j] *= f;
-    }
-#pragma unroll
-    for (int st = 0; st < SUB; ++st)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        z[st][i] = __builtin_amdgcn_exp2f(z[st][i] - mref);
-        l += z[st][i];
-      }
-    if constexpr (BF16) {
-      // A weight enters as the sum of two bfloat16 numbers, 16 bits of mantissa: one alone would add half of the output's own
-      // rounding to its error, and the matrix units are idle most of the time.
-      uint32_t hi[2 * SUB], lo[2 * SUB];
-#pragma unroll
-      for (int i = 0; i < 2 * SUB; ++i) {
-        const float p0 = z[i / 2][i % 2 * 2], p1 = z[i / 2][i % 2 * 2 + 1];
-        hi[i] = pack_bf16(p0, p1);
-        lo[i] = pack_bf16(p0 - __uint_as_float(hi[i] << 16), p1 - __uint_as_float(hi[i] & 0xffff0000u));
-      }
-#pragma unroll
-      for (int blk = 0; blk < NBLK; ++blk)
-#pragma unroll
-        for (int j = 0; j < EPL; ++j) {
-          uint32_t vt[2 * SUB];
-#pragma unroll
-          for (int i = 0; i < 2 * SUB; ++i)
-            vt[i] = __builtin_amdgcn_perm(vr[2 * i + 1][blk][j / 2], vr[2 * i][blk][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
-          o[blk][j] = weighted<SUB>(vt, hi, o[blk][j]);
-          o[blk][j] = weighted<SUB>(vt, lo, o[blk][j]);
+        for (int blk = 0; blk < NBLK; ++blk) {
+          const char* p = row + blk * (BD * sizeof(X));
+          if (!FULL && (blk * 16 + m16) * EPL >= a.D) p = zeros;
+          vr[u][blk] = read<NT, VWord>(p);
         }
-    } else {
-#pragma unroll
-      for (int blk = 0; blk < NBLK; ++blk)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < EPL; ++j)
-            o[blk][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[i][blk][j]), z[0][i], o[blk][j], 0, 0, 0);
-    }
-    load_values();
-    t += step;
-  } while (t < t_end);
-  }
+      }
+    };
 
-  // the wavefronts' parts: common maximum, then the sum through LDS
-  l += __shfl_xor(l, 16, 64);
-  l += __shfl_xor(l, 32, 64);
-  lds_barrier();  // (the piece before has been read)
-  if (g == 0) ml_lds[wave][m16] = f32x2{m, l};
-  lds_barrier();
-  // (wavefront w and those a multiple of wave_heads away have the same kv head)
-  auto joined_max = [&](int w, int row) {
-    float top = -INFINITY;
-    for (w &= wave_heads - 1; w < WAVES; w += wave_heads) top = fmaxf(top, ml_lds[w][row][0]);
-    return top;
-  };
-  auto part_weight = [&](int w, int row, float top) { return top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml_lds[w][row][0] - top); };
-  const float f = m16 < my_heads ? part_weight(wave, m16, joined_max(wave, m16)) : 0.f;
-  const int d = threadIdx.x % (BD / 4) * 4;
+    float m = -INFINITY, mref = 0.f, l = 0.f;
+    f32x4 o[NBLK][EPL];
 #pragma unroll
-  for (int blk = 0; blk < NBLK; ++blk) {
-    if (blk) lds_barrier();
-    if (m16 < my_heads) {
-      float* row = o_lds + (wave * a.rows + m16) * PITCH;
+    for (int blk = 0; blk < NBLK; ++blk)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int j = 0; j < EPL; ++j) o[blk][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    if (t < t_end) {
+      u32x4 qr[KSTEPS];
+      const bool have = m16 < my_heads;
+      const char* q_row = a.q + (int64_t)b * a.q_token + (int64_t)(hk * a.G + ht * HEADS + m16) * a.q_head + g * 16;
 #pragma unroll
-        for (int j = 0; j < EPL; j += 4)
-          *reinterpret_cast<f32x4*>(row + (g * 4 + i) * EPL + j) =
-              f32x4{o[blk][j][i] * f, o[blk][j + 1][i] * f, o[blk][j + 2][i] * f, o[blk][j + 3][i] * f};
+      for (int s = 0; s < KSTEPS; ++s) qr[s] = read<false, u32x4>(have && (s * 64 + g * 16) < a.D * (int)sizeof(X) ? q_row + s * 64 : zeros);
+      if (!early) {
+        now = entry_of(t);
+        entry = entry_of(t + step);
+      }
+      uint32_t kept = place_rows(t, now);
+      __builtin_amdgcn_sched_barrier(0);  // (the loop counts on the keys being requested first)
+      load_keys();
+      __builtin_amdgcn_sched_barrier(0);
+      load_values();
+      do {
+        const uint32_t here = kept;
+        const int entry_next = entry_of(t + 2 * step);
+        f32x4 z[SUB];
+#pragma unroll
+        for (int st = 0; st < SUB; ++st) {
+          // [e][h]: keys e*8.. by the pieces 4h..4h+3 of their lines; rows 8h..8h+7 of the product are the ones that mean something
+          f32x4 part[2][2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              part[e][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+              for (int c = 0; c < LINES; ++c) part[e][h] = product<BF16>(kr[st][e][c], qr[2 * c + h], part[e][h]);
+            }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            // a place's other half lies 32 lanes away
+            const float mine = lane < 32 ? part[0][0][i] : part[1][1][i], other = lane < 32 ? part[1][0][i] : part[0][1][i];
+            z[st][i] = mine + other_half(other, lane);
+          }
+        }
+        kept = place_rows(t + step, entry);
+        entry = entry_next;
+        load_keys();
+        // scores in units of log 2
+        if (plain) {
+#pragma unroll
+          for (int st = 0; st < SUB; ++st) z[st] *= scale2;
+        } else {
+#pragma unroll
+          for (int st = 0; st < SUB; ++st)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float s = z[st][i] * a.scale;
+              if (a.cap > 0.f) s = a.cap * tanhf(s * a.inv_cap);
+              s -= slope * (float)(n - 1 - (t * TILE + st * 16 + g * 4 + i));
+              z[st][i] = s * LOG2E;
+            }
+        }
+        if (here != EVERY) {
+#pragma unroll
+          for (int st = 0; st < SUB; ++st)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (!((here >> (st * 16 + g * 4 + i)) & 1)) z[st][i] = -INFINITY;
+        }
+        float top = z[0][0];
+#pragma unroll
+        for (int st = 0; st < SUB; ++st)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) top = fmaxf(top, z[st][i]);
+        // The maximum moves only when some score passes it by a factor of 2^8: until then the weights grow to at most that, which
+        // float32 sums do not mind, and the four lanes of a head need not exchange theirs.
+        if (__any(top > m + 8.f)) {
+          top = fmaxf(top, __shfl_xor(top, 16, 64));
+          top = fmaxf(top, __shfl_xor(top, 32, 64));
+          const float now = fmaxf(m, top), f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - now);
+          m = now;
+          mref = now == -INFINITY ? 0.f : now;
+          l *= f;
+#pragma unroll
+          for (int blk = 0; blk < NBLK; ++blk)
+#pragma unroll
+            for (int j = 0; j < EPL; ++j) o[blk][j] *= f;
+        }
+#pragma unroll
+        for (int st = 0; st < SUB; ++st)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            z[st][i] = __builtin_amdgcn_exp2f(z[st][i] - mref);
+            l += z[st][i];
+          }
+        if constexpr (BF16) {
+          // A weight enters as the sum of two bfloat16 numbers, 16 bits of mantissa: one alone would add half of the output's own
+          // rounding to its error, and the matrix units are idle most of the time.
+          uint32_t hi[2 * SUB], lo[2 * SUB];
+#pragma unroll
+          for (int i = 0; i < 2 * SUB; ++i) {
+            const float p0 = z[i / 2][i % 2 * 2], p1 = z[i / 2][i % 2 * 2 + 1];
+            hi[i] = pack_bf16(p0, p1);
+            lo[i] = pack_bf16(p0 - __uint_as_float(hi[i] << 16), p1 - __uint_as_float(hi[i] & 0xffff0000u));
+          }
+#pragma unroll
+          for (int blk = 0; blk < NBLK; ++blk)
+#pragma unroll
+            for (int j = 0; j < EPL; ++j) {
+              uint32_t vt[2 * SUB];
+#pragma unroll
+              for (int i = 0; i < 2 * SUB; ++i)
+                vt[i] = __builtin_amdgcn_perm(vr[2 * i + 1][blk][j / 2], vr[2 * i][blk][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+              o[blk][j] = weighted<SUB>(vt, hi, o[blk][j]);
+              o[blk][j] = weighted<SUB>(vt, lo, o[blk][j]);
+            }
+        } else {
+#pragma unroll
+          for (int blk = 0; blk < NBLK; ++blk)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int j = 0; j < EPL; ++j)
+                o[blk][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[i][blk][j]), z[0][i], o[blk][j], 0, 0, 0);
+        }
+        load_values();
+        t += step;
+      } while (t < t_end);
     }
+
+    // the wavefronts' parts: common maximum, then the sum through LDS
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    lds_barrier();  // (the piece before has been read)
+    if (g == 0) ml_lds[wave][m16] = f32x2{m, l};
     lds_barrier();
-    const int dim = blk * BD + d;
-    for (int i = threadIdx.x / (BD / 4); i < a.rows * wave_heads; i += 64 * WAVES / (BD / 4)) {
-      const int wh = a.per_rows.quotient(i), r = i - wh * a.rows, its = at.first_item + wh;  // the row's item
-      const int its_hk = a.per_kv_head.quotient(its), its_ht = its - its_hk * a.hts;
-      if (r >= heads_of(its_ht)) continue;
-      const float top = joined_max(wh, r);
-      float sum = 0.f;
-      f32x4 y{0.f, 0.f, 0.f, 0.f};
-      for (int w = wh; w < WAVES; w += wave_heads) {
-        sum += ml_lds[w][r][1] * part_weight(w, r, top);
-        y += *reinterpret_cast<const f32x4*>(o_lds + (w * a.rows + r) * PITCH + d);
+    // (wavefront w and those a multiple of wave_heads away have the same kv head)
+    auto joined_max = [&](int w, int row) {
+      float top = -INFINITY;
+      for (w &= wave_heads - 1; w < WAVES; w += wave_heads) top = fmaxf(top, ml_lds[w][row][0]);
+      return top;
+    };
+    auto part_weight = [&](int w, int row, float top) { return top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml_lds[w][row][0] - top); };
+    const float f = m16 < my_heads ? part_weight(wave, m16, joined_max(wave, m16)) : 0.f;
+    const int d = threadIdx.x % (BD / 4) * 4;
+#pragma unroll
+    for (int blk = 0; blk < NBLK; ++blk) {
+      if (blk) lds_barrier();
+      if (m16 < my_heads) {
+        float* row = o_lds + (wave * a.rows + m16) * PITCH;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < EPL; j += 4)
+            *reinterpret_cast<f32x4*>(row + (g * 4 + i) * EPL + j) =
+                f32x4{o[blk][j][i] * f, o[blk][j + 1][i] * f, o[blk][j + 2][i] * f, o[blk][j + 3][i] * f};
       }
-      if (!FULL && dim >= a.D) continue;
-      if (whole) {
-        store_row<X>(a, b, its_hk * a.G + its_ht * HEADS + r, dim, y, sum, top);
-      } else {
-        const int64_t part = ((int64_t)slot * a.items + its) * a.rows + r;
-        *reinterpret_cast<f32x4*>(a.part_o + part * a.D + dim) = y;
-        if (dim == 0) a.part_ml[part] = f32x2{top, sum};
+      lds_barrier();
+      const int dim = blk * BD + d;
+      for (int i = threadIdx.x / (BD / 4); i < a.rows * wave_heads; i += 64 * WAVES / (BD / 4)) {
+        const int wh = a.per_rows.quotient(i), r = i - wh * a.rows, its = at.first_item + wh;  // the row's item
+        const int its_hk = a.per_kv_head.quotient(its), its_ht = its - its_hk * a.hts;
+        if (r >= heads_of(its_ht)) continue;
+        const float top = joined_max(wh, r);
+        float sum = 0.f;
+        f32x4 y{0.f, 0.f, 0.f, 0.f};
+        for (int w = wh; w < WAVES; w += wave_heads) {
+          sum += ml_lds[w][r][1] * part_weight(w, r, top);
+          y += *reinterpret_cast<const f32x4*>(o_lds + (w * a.rows + r) * PITCH + d);
+        }
+        if (!FULL && dim >= a.D) continue;
+        if (whole) {
+          store_row<X>(a, b, its_hk * a.G + its_ht * HEADS + r, dim, y, sum, top);
+        } else {
+          const int64_t part = ((int64_t)slot * a.items + its) * a.rows + r;
+          *reinterpret_cast<f32x4*>(a.part_o + part * a.D + dim) = y;
+          if (dim == 0) a.part_ml[part] = f32x2{top, sum};
+        }
       }
     }
-  }
-  x = b_end;
-  at.begin = b_end;
-  if (x < x_end) at.len = a.lens[++at.b];
+    x = b_end;
+    at.begin = b_end;
+    if (x < x_end) at.len = a.lens[++at.b];
   }
 }
 
@@ -583,8 +602,9 @@ Split split_of(const moe_kv_cache* c, int32_t n_q_heads, int32_t window) {
   const int G = n_q_heads / c->n_kv_heads, es = (int)elem_size(c->dtype), tile = es == 2 && c->head_dim <= 128 ? 32 : 16;
   s.rows = G < HEADS ? G : HEADS;
   s.items = c->n_kv_heads * ((G + HEADS - 1) / HEADS);
-  // Neighbouring items by one workgroup: tiles of query heads that read the same keys and values, and kv heads whose rows are
-  // neighbours in memory.
+  // Neighbouring items by one workgroup: tiles of query heads that read the same keys and values (64 heads on one kv head 104 us
+  // apart, 83 together), and kv heads whose rows are neighbours in memory, 512 bytes of them (256-byte rows, 8.5 GB: 1334 us one by
+  // one, 1263 by twos, 1308 by fours; 128-byte rows: 107, 100 and 93).
   const bool several = s.items > c->n_kv_heads, neighbours = c->head_stride < c->token_stride;
   const int wanted = several ? 4 : !neighbours ? 1 : c->head_dim * es <= 128 ? 4 : 2;
   s.wave_heads = s.items % wanted == 0 ? wanted : s.items % 2 == 0 && wanted > 1 ? 2 : 1;
@@ -606,6 +626,8 @@ Split split_of(const moe_kv_cache* c, int32_t n_q_heads, int32_t window) {
     const int wave_heads = kept > TINY_PLACES ? s.wave_heads : s.items % 4 == 0 ? 4 : s.items % 2 == 0 ? 2 : 1;
     s.grid = (int)(work / wave_heads);
   }
+  // Pools that the last-level cache (256 MB) cannot keep for the next call are read past it: 537 MB 99 us, 107 through the caches; of
+  // 79 MB that it keeps 27 and 24.
   s.nt = (double)c->n_pages * c->page_size * c->n_kv_heads * c->head_dim * 2 * es > (double)(300 << 20);
   s.ml = align_up((size_t)c->n_seqs * sizeof(int2), 256);
   s.o = s.ml + align_up((size_t)s.parts * 2 * s.items * s.rows * sizeof(f32x2), 256);
