@@ -77,7 +77,7 @@ struct DecodeArgs {
     int32_t parts;
     double inverse_parts;
   } share_of_grid[3];  // with 1, 2 and 4 items a workgroup
-  int32_t page_size, table_width, capacity, n_seqs, hq, hkv, G, rows, items, hts, log_heads, parts, may_split, D, window, least;
+  int32_t page_size, table_width, capacity, n_seqs, hq, G, rows, items, hts, log_heads, parts, may_split, D, window, least;
   float scale, cap, inv_cap;
 };
 
@@ -727,7 +727,6 @@ extern "C" int32_t moe_attention_decode(const moe_kv_cache* c, int32_t n_q_heads
   a.table_width = c->table_width;
   a.n_seqs = c->n_seqs;
   a.hq = n_q_heads;
-  a.hkv = c->n_kv_heads;
   a.G = n_q_heads / c->n_kv_heads;
   a.rows = sp.rows;
   a.items = sp.items;

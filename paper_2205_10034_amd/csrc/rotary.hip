@@ -138,10 +138,11 @@ __global__ __launch_bounds__(64 * WAVES) void token_kernel(TokenArgs a) {
         // in float64, reduced to one turn: in float32 the angle of position 10^6 would be off by 0.06
         double turns = (double)a.positions[(int64_t)axis * a.T + t] * a.freqs[i] * 0.15915494309189533577;
         turns -= rint(turns);
+        const float near = (float)turns, off = 6.2831853f * (float)(turns - near);  // what rounding to float32 took, in radians
         float s, c;
-        sincospif(2.0f * (float)turns, &s, &c);
-        cosine[wave][i] = c;
-        sine[wave][i] = a.sign * s;
+        sincospif(2.0f * near, &s, &c);
+        cosine[wave][i] = c - s * off;
+        sine[wave][i] = a.sign * (s + c * off);
       }
       asm volatile("" ::: "memory");  // (a wavefront's LDS operations execute in order)
     }
