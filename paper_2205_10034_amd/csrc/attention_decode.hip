@@ -105,7 +105,7 @@ __device__ __forceinline__ int64_t uniform(int64_t v, int lane) {
   return (int64_t)(((uint64_t)hi << 32) | lo);
 }
 
-// How the workgroups share the batch, from its lengths: a wavefront's place in it.  Every wavefront finds it by itself.
+// How the workgroups share the batch, from its lengths, and this one's part of it.  Every wavefront finds it by itself.
 struct Deal {
   int log_heads, first_item, w;  // items of a workgroup (their logarithm), the first of them, the part
   bool one_each;              // the row counts sequences, not tiles: no sequence is split
@@ -150,7 +150,7 @@ __device__ __forceinline__ Deal deal(const DecodeArgs& a, int tile) {
   if (tiny || (small && rows <= grid)) return whole();
   for (int d = 1; d < 64 && d < a.n_seqs; d <<= 1) total += __shfl_xor(total, d, 64);
   p.total = uniform(total, 0);
-  take(p.total * tile < (int64_t)a.n_seqs * SMALL_PLACES && rows >= 2 * grid ? side_by_side(a.items, rows, grid) : a.log_heads);
+  take(a.log_heads);
   p.share = uniform(share_of_row(p.total, a.share_of_grid[p.log_heads].inverse_parts, a.least >> p.log_heads), 0);
   const int64_t at = p.w * p.share;
   if (at >= p.total) return p;
@@ -226,7 +226,8 @@ __device__ __forceinline__ void store_row(const DecodeArgs& a, int b, int h, int
   if (a.lse && d == 0) a.lse[(int64_t)b * a.hq + h] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
 }
 
-// One (sequence, kv head, tile of query heads, chunk of places) per workgroup; its wavefronts take the chunk's tiles in turn.
+// A part of the batch per workgroup, piece after piece; its wavefronts take an item's tiles in turn.  An item is a kv head and up to 16
+// of its query heads.
 // FULL: head_dim is DP, no lane's dimensions lie beyond it.
 template <typename X, int DP, bool FULL, bool NT>
 __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) void decode_kernel(DecodeArgs a) {
@@ -302,7 +303,7 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) voi
 
     u32x4 kr[SUB][2][LINES];
     VWord vr[NV][NBLK];
-    // 8 keys' whole 128-byte lines per instruction: lane (m16, g) has piece g + 4 (m16 / 8) of key m16 % 8
+    // 8 keys' whole 128-byte lines per instruction: lane (m16, g) has the g + 4 (m16 / 8)-th 16 bytes of key m16 % 8's
     auto load_keys = [&]() {
 #pragma unroll
       for (int st = 0; st < SUB; ++st)
@@ -358,7 +359,7 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) voi
         f32x4 z[SUB];
 #pragma unroll
         for (int st = 0; st < SUB; ++st) {
-          // [e][h]: keys e*8.. by the pieces 4h..4h+3 of their lines; rows 8h..8h+7 of the product are the ones that mean something
+          // [e][h]: keys e*8.. by the halves h of their lines; rows 8h..8h+7 of the product are the ones that mean something
           f32x4 part[2][2];
 #pragma unroll
           for (int e = 0; e < 2; ++e)
