@@ -109,6 +109,7 @@ __device__ __forceinline__ int64_t uniform(int64_t v, int lane) {
 struct Deal {
   int log_heads, first_item, w;  // items of a workgroup (their logarithm), the first of them, the part
   bool one_each;              // the row counts sequences, not tiles: no sequence is split
+  bool aligned;               // every sequence begins a part
   int64_t share, total;       // of a part, of the row
   int64_t begin;              // where in the row sequence b begins
   int b, len;                 // the part's first sequence, its length
@@ -131,7 +132,7 @@ __device__ __forceinline__ Deal deal(const DecodeArgs& a, int tile) {
     take(side_by_side(a.items, rows, grid));
     const auto& g = a.share_of_grid[p.log_heads];
     p.one_each = true;
-    p.share = (int64_t)(((double)(a.n_seqs + g.parts) - 0.5) * g.inverse_parts);  // rounded up: half a unit from where the product's rounding could matter
+    p.share = share_of_row(a.n_seqs, g.inverse_parts, 1);
     p.total = a.n_seqs;
     p.begin = p.w * p.share;
     p.b = (int)p.begin;
@@ -152,9 +153,16 @@ __device__ __forceinline__ Deal deal(const DecodeArgs& a, int tile) {
   p.total = uniform(total, 0);
   take(a.log_heads);
   p.share = uniform(share_of_row(p.total, a.share_of_grid[p.log_heads].inverse_parts, a.least >> p.log_heads), 0);
+  // A piece costs its trips to memory, about what a tile of every wavefront costs where all of them read: for up to that much a
+  // part, sequences begin parts of their own and no part holds two pieces.
+  if (a.n_seqs > 1 && a.n_seqs < a.share_of_grid[p.log_heads].parts) {
+    const int64_t wider = uniform(share_of_row(p.total, 1.0 / (a.share_of_grid[p.log_heads].parts - a.n_seqs), a.least >> p.log_heads), 0);
+    p.aligned = wider - p.share <= (WAVES >> p.log_heads);
+    if (p.aligned) p.share = wider;
+  }
   const int64_t at = p.w * p.share;
-  if (at >= p.total) return p;
-  for (int s = 0;;) {
+  for (int s = 0; s < a.n_seqs;) {
+    if (p.aligned) mine = aligned_tiles(mine, p.share);
     int64_t upto = mine;
     for (int d = 1; d < 64 && d < a.n_seqs; d <<= 1) {
       const int64_t other = __shfl_up(upto, d, 64);
@@ -166,6 +174,7 @@ __device__ __forceinline__ Deal deal(const DecodeArgs& a, int tile) {
       p.b = s + who;
       p.len = __builtin_amdgcn_readlane(len, who);
       p.begin += uniform(upto - mine, who);
+      if (p.aligned) p.total = at + p.share;  // (this part's end will do)
       return p;
     }
     p.begin += uniform(upto, 63);
@@ -173,6 +182,8 @@ __device__ __forceinline__ Deal deal(const DecodeArgs& a, int tile) {
     len = s + lane < a.n_seqs ? a.lens[s + lane] : 0;
     mine = s + lane < a.n_seqs ? row_tiles(tiles_in(len)) : 0;
   }
+  p.total = 0;  // nothing is left for this part
+  return p;
 }
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -276,7 +287,7 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) voi
       entry = entry_of(mine + step);
     }
     const int n = kept_length(at.len, a.capacity), first = first_place(n, a.window), tile0 = first / TILE, tiles = kept_tiles(n, first, TILE);
-    const int64_t b_end = at.begin + (at.one_each ? 1 : row_tiles(tiles));
+    const int64_t b_end = at.begin + (at.one_each ? 1 : at.aligned ? aligned_tiles(row_tiles(tiles), at.share) : row_tiles(tiles));
     const int upto = b_end <= x_end ? tiles : (int)(x_end - at.begin);
     const bool whole = from == 0 && b_end <= x_end;
     const int slot = 2 * w + (piece_no > 0);

@@ -38,12 +38,14 @@ inline PageDivisor page_divisor(int d) {
 // (somebody has to write its zeros); part w of the row is the tiles w*share .. (w+1)*share - 1.  A part holds pieces of one or more
 // sequences; a sequence that lies in one part is finished there, the pieces of the others are joined.
 MOESYS_HD int64_t row_tiles(int tiles) { return tiles > 0 ? tiles : 1; }
-// Tiles of a part: enough that `parts` of them hold the row (inverse = 1.0 / parts; floor + 1 is at least the quotient rounded up,
-// whichever way the product was rounded), at least `least`.
+// Tiles of a part: total / parts rounded up, which `parts` of them hold the row with, at least `least`.  inverse = 1.0 / parts; half a
+// tile below, the product is further from a whole number than its rounding reaches.
 MOESYS_HD int64_t share_of_row(int64_t total, double inverse, int least) {
-  const int64_t share = (int64_t)((double)total * inverse) + 1;
+  const int64_t share = (int64_t)(((double)total - 0.5) * inverse) + 1;
   return share < least ? least : share;
 }
+// A sequence's place in a row where sequences begin parts: whole shares.  (Tiles and shares are below 2^31.)
+MOESYS_HD int64_t aligned_tiles(int64_t tiles, int64_t share) { return (int64_t)(((uint32_t)tiles + (uint32_t)share - 1u) / (uint32_t)share) * share; }
 // Part that tile `at` of the row lies in; the quotient in float64 is off by one at most.
 MOESYS_HD int part_of(int64_t at, int64_t share) {
   int64_t w = (int64_t)((double)at / (double)share);

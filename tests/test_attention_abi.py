@@ -209,8 +209,17 @@ int main() {
     std::vector<long long> tiles(S);
     long long total = 0;
     for (long long& t : tiles) { t = row_tiles(next() % 5 ? (int)(next() % (cap + 1)) : 0); assert(t >= 1); total += t; }
-    const long long share = share_of_row(total, 1.0 / parts, least);
+    long long share = share_of_row(total, 1.0 / parts, least);
     assert(share >= least && share * parts >= total);
+    const long long really = total;
+    const std::vector<long long> held = tiles;
+    const bool aligned = round % 3 == 1 && S < parts;
+    if (aligned) {  // sequences begin parts: places of whole shares, which the parts still hold
+      share = share_of_row(total, 1.0 / (parts - S), least);
+      total = 0;
+      for (long long& t : tiles) { const long long was = t; t = aligned_tiles(t, share); assert(t >= was && t - was < share && t % share == 0); total += t; }
+      assert(total <= share * parts);
+    }
     // the parts walk over the row as the kernel does; every piece but whole ones has a slot of its own, where the join looks
     std::vector<int> pieces(S, 0), first(S, -1), used(2 * parts, -1);
     long long covered = 0;
@@ -222,6 +231,7 @@ int main() {
       for (int no = 0; x < x_end; ++no) {
         const long long b_end = begin + tiles[b], stop = b_end < x_end ? b_end : x_end;
         const bool whole = x == begin && b_end <= x_end;
+        assert(!aligned || no == 0);
         const int slot = 2 * w + (no > 0);
         if (x == begin) {
           first[b] = slot;
@@ -232,21 +242,21 @@ int main() {
         if (!whole) { assert(used[slot] < 0); used[slot] = b; }
         const int j = w - first[b] / 2;
         assert(first[b] >= 0 && piece_slot(first[b], j) == slot && j < -pieces[b]);
-        covered += stop - x;
+        covered += aligned ? (b_end <= x_end ? held[b] : x_end - begin) - (x - begin) : stop - x;
         if (b_end <= x_end) assert(j == -pieces[b] - 1);
         x = b_end; begin = b_end; ++b;
       }
     }
-    assert(covered == total);
+    assert(covered == really);
   }
   for (int i = 0; i < 200000; ++i) {
     const long long share = 1 + next() % (i % 2 ? 50 : 1 << 24), part = next() % 2000;
     for (int e = -1; e < 2; ++e) if (part * share + e >= 0) assert(part_of(part * share + e, share) == (part * share + e) / share);
     // sequences of a part, as the kernel rounds them up
     const int S = 1 + next() % (i % 3 ? 600 : 1 << 30), parts = 1 + next() % (i % 5 ? 2048 : 1 << 20);
-    assert((long long)(((double)(S + parts) - 0.5) * (1.0 / parts)) == ((long long)S + parts - 1) / parts);
+    assert(share_of_row(S, 1.0 / parts, 1) == ((long long)S + parts - 1) / parts);
   }
   // the quotient in float64, at its worst
   for (long long total : {1ll, 2ll, 3ll, 1000000007ll, (1ll << 40) - 1, 1ll << 40, (1ll << 40) + 1})
-    for (int parts = 1; parts < 3000; ++parts) assert(share_of_row(total, 1.0 / parts, 1) * parts >= total);
+    for (int parts = 1; parts < 3000; ++parts) assert(share_of_row(total, 1.0 / parts, 1) == (total + parts - 1) / parts);
 }""")
