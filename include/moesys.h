@@ -615,8 +615,8 @@ typedef struct {
  *   lse = log sum_j exp(z_j)        out_h = sum_j exp(z_j - lse) v_j
  * No place kept, or no score above -infinity: out_h = 0, lse = -infinity.  What lies in places that are not kept (NaN
  * and infinities among it) reaches no output; an infinite value in a kept place makes its element of out infinite or NaN.
- * Products of MOE_BF16 are exact and accumulated in float32, softmax
- * weights enter with 16 bits of mantissa, out is rounded once.
+ * Products of MOE_BF16 are exact and accumulated in float32, softmax weights are float32 numbers with all their bits,
+ * out is rounded once.
  * q, out [n_seqs, n_q_heads, head_dim], pointers and strides multiples of 16 bytes; n_q_heads a multiple of
  * n_kv_heads; lse (nullable) device float [n_seqs, n_q_heads].  ws: moe_attention_decode_workspace_bytes, 256-byte
  * aligned, need not be cleared, one call at a time.  Results do not depend on what else runs: the split over the

@@ -439,14 +439,19 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) voi
             l += z[st][i];
           }
         if constexpr (BF16) {
-          // A weight enters as the sum of two bfloat16 numbers, 16 bits of mantissa: one alone would add half of the output's own
-          // rounding to its error, and the matrix units are idle most of the time.
-          uint32_t hi[2 * SUB], lo[2 * SUB];
+          // A weight enters as the sum of three bfloat16 numbers, each the leading 8 bits of what the ones before leave: all of its 24.
+          // (With two, 16 to 17 bits, outputs whose values cancel over a long cache carried three times the error of a 32-bit sum.)
+          uint32_t weight[3][2 * SUB];
 #pragma unroll
           for (int i = 0; i < 2 * SUB; ++i) {
-            const float p0 = z[i / 2][i % 2 * 2], p1 = z[i / 2][i % 2 * 2 + 1];
-            hi[i] = pack_bf16(p0, p1);
-            lo[i] = pack_bf16(p0 - __uint_as_float(hi[i] << 16), p1 - __uint_as_float(hi[i] & 0xffff0000u));
+            float p0 = z[i / 2][i % 2 * 2], p1 = z[i / 2][i % 2 * 2 + 1];
+#pragma unroll
+            for (int s = 0; s < 3; ++s) {
+              const uint32_t u0 = __float_as_uint(p0), u1 = __float_as_uint(p1);
+              weight[s][i] = __builtin_amdgcn_perm(u1, u0, 0x07060302u);
+              p0 -= __uint_as_float(u0 & 0xffff0000u);
+              p1 -= __uint_as_float(u1 & 0xffff0000u);
+            }
           }
 #pragma unroll
           for (int blk = 0; blk < NBLK; ++blk)
@@ -456,8 +461,8 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) voi
 #pragma unroll
               for (int i = 0; i < 2 * SUB; ++i)
                 vt[i] = __builtin_amdgcn_perm(vr[2 * i + 1][blk][j / 2], vr[2 * i][blk][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
-              o[blk][j] = weighted<SUB>(vt, hi, o[blk][j]);
-              o[blk][j] = weighted<SUB>(vt, lo, o[blk][j]);
+#pragma unroll
+              for (int s = 0; s < 3; ++s) o[blk][j] = weighted<SUB>(vt, weight[s], o[blk][j]);
             }
         } else {
 #pragma unroll

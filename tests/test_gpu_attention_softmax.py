@@ -1,0 +1,34 @@
+"""Softmax of the decode attention where its arithmetic shows: outputs that cancel."""
+import numpy as np
+import pytest
+import torch
+
+from attention_util import DT, HALF_STEP, Paged, attend
+from oracle import attention_oracle as A
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 64), ("bf16", 128), ("bf16", 256), ("f32", 64), ("f32", 256)])
+def test_weights_keep_the_bits_of_float32(dtype, D):
+    """Three keys with scores a, a + 2^-12 and a + t and values -1, 1 and 0: out = (w1 - w0) / sum w, some 2^-14, lays the weights'
+    own errors bare.  Scores are exact, at most 2; every other step of a weight (scale, difference to the maximum, change to powers of
+    two) rounds 2^-24 |z| or less each, 6 * 2^-24 together, the power itself is good to 2^-23, the sums of three to 2 * 2^-24: at most
+    10 * 2^-24 of a weighted mean of |v| that is below 1.  Then one rounding."""
+    S = 96
+    p = Paged([3] * S, 1, D, 4, dtype)
+    rng = np.random.default_rng(7)
+    a, t = rng.integers(0, 128, S) / 128.0, rng.integers(1, 128, S) / 128.0
+    p.k[p.table[:, 0], :3] = p.v[p.table[:, 0], :3] = 0.0
+    page = p.table[:, 0]
+    p.k[page, :3, 0, 0] = a[:, None]
+    p.k[page, 1, 0, 1], p.k[page, 2, 0, 1] = 2.0 ** -12, t
+    p.v[page, 0], p.v[page, 1] = -1.0, 1.0
+    q = torch.zeros(S, 2, D)
+    q[:, :, :2] = 1.0
+    q = q.to(DT[dtype])
+    out, lse = attend(p.cache(), q, p.lens, scale=1.0)
+    ref, ref_lse, mean_abs, *_ = A.decode(p.k, p.v, p.table, q.float().numpy(), p.lens, 1.0)
+    off, tol = np.abs(out - ref), 10 * 2.0 ** -24 * mean_abs + HALF_STEP[dtype] * 1.01 * np.abs(ref)
+    assert (off <= tol).all(), f"{(off > tol).sum()} of {off.size} off, by up to {(off / tol).max():.1f} times what is allowed"
+    assert np.abs(lse - ref_lse).max() <= 16 * 2.0 ** -24 * 4
