@@ -50,6 +50,8 @@ constexpr int MANY_ROWS = 1024;
 // places 7 us and 12, 16 of up to 1000 places 15.4 and 18.1, 512 of up to 700 131 and 140; 256 of up to 2000 are better shared,
 // 171 against 186).
 constexpr int TINY_PLACES = 128, SMALL_PLACES = 1024;
+// How far a score may pass the running maximum, as a power of two, before the maximum moves; weights are scaled down by as much.
+constexpr int LAG_BITS = 8;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 // Rows of places that are not there and dimensions beyond head_dim are read from here: no load leaves the caller's rows, and what
@@ -234,7 +236,7 @@ __device__ __forceinline__ void store_row(const DecodeArgs& a, int b, int h, int
   char* p = a.out + (int64_t)b * a.o_token + (int64_t)h * a.o_head + d * sizeof(X);
   if constexpr (sizeof(X) == 2) *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
   else *reinterpret_cast<f32x4*>(p) = y;
-  if (a.lse && d == 0) a.lse[(int64_t)b * a.hq + h] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
+  if (a.lse && d == 0) a.lse[(int64_t)b * a.hq + h] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum * (1 << LAG_BITS))) * LN2;
 }
 
 // A part of the batch per workgroup, piece after piece; its wavefronts take an item's tiles in turn.  An item is a kv head and up to 16
@@ -417,9 +419,10 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) voi
         for (int st = 0; st < SUB; ++st)
 #pragma unroll
           for (int i = 0; i < 4; ++i) top = fmaxf(top, z[st][i]);
-        // The maximum moves only when some score passes it by a factor of 2^8: until then the weights grow to at most that, which
-        // float32 sums do not mind, and the four lanes of a head need not exchange theirs.
-        if (__any(top > m + 8.f)) {
+        // The maximum moves only when some score passes it by a factor of 2^8, so that the four lanes of a head need not exchange
+        // theirs.  All weights are 2^-8 of what they would be (sums, and so lse, with them): none is above 1, and no product with a
+        // finite value overflows.
+        if (__any(top > m + (float)LAG_BITS)) {
           top = fmaxf(top, __shfl_xor(top, 16, 64));
           top = fmaxf(top, __shfl_xor(top, 32, 64));
           const float now = fmaxf(m, top), f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - now);
@@ -435,7 +438,7 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) voi
         for (int st = 0; st < SUB; ++st)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            z[st][i] = __builtin_amdgcn_exp2f(z[st][i] - mref);
+            z[st][i] = __builtin_amdgcn_exp2f(z[st][i] - mref) * (1.f / (1 << LAG_BITS));
             l += z[st][i];
           }
         if constexpr (BF16) {

@@ -1,4 +1,4 @@
-"""Softmax of the decode attention where its arithmetic shows: outputs that cancel."""
+"""Softmax of the decode attention where its arithmetic shows: outputs that cancel, values and scores near the ends of float32."""
 import numpy as np
 import pytest
 import torch
@@ -32,3 +32,31 @@ def test_weights_keep_the_bits_of_float32(dtype, D):
     off, tol = np.abs(out - ref), 10 * 2.0 ** -24 * mean_abs + HALF_STEP[dtype] * 1.01 * np.abs(ref)
     assert (off <= tol).all(), f"{(off > tol).sum()} of {off.size} off, by up to {(off / tol).max():.1f} times what is allowed"
     assert np.abs(lse - ref_lse).max() <= 16 * 2.0 ** -24 * 4
+
+
+@pytest.mark.parametrize("dtype,D,far", [("bf16", 64, 128), ("bf16", 256, 64), ("f32", 64, 64), ("f32", 256, 64)])
+def test_large_values_under_rising_scores(dtype, D, far):
+    """Values near the type's largest whose keys are a little better than those before them: the mean of finite values is finite.
+    All scores are equal but one, 5.4 higher (a factor of 222), in place `far`, a tile that the same wavefront takes later.  Scores
+    are exact and below 6, so weights are off by 64 * 2^-24 at most (scale, differences, exponent on |z| < 8, the power), sums of
+    n by n * 2^-24."""
+    lens = [129, 200, 257, 1000, 3000]
+    p = Paged(lens, 1, D, 16, dtype)
+    big = torch.tensor(3e38).to(DT[dtype]).item()
+    for s, n in enumerate(lens):
+        for i in range(-(-n // 16)):
+            rows = min(16, n - i * 16)
+            p.k[p.table[s, i], :rows], p.v[p.table[s, i], :rows] = 0.0, 1.0
+        at = (p.table[s, far // 16], 0, 0)
+        p.k[at][0], p.v[at][:] = 5.40625, big
+        p.v[at][1::2] = -big
+    q = torch.zeros(len(lens), 3, D)
+    q[:, :, 0] = 1.0
+    q = q.to(DT[dtype])
+    out, lse = attend(p.cache(), q, p.lens, scale=1.0)
+    ref, ref_lse, mean_abs, *_ = A.decode(p.k, p.v, p.table, q.float().numpy(), p.lens, 1.0)
+    lost = int((~np.isfinite(out)).sum())
+    assert lost == 0, f"{lost} of {out.size} are not finite"
+    tol = (64 + np.array(lens))[:, None, None] * 2.0 ** -24 * mean_abs + HALF_STEP[dtype] * 1.01 * np.abs(ref)
+    assert (np.abs(out - ref) <= tol).all()
+    assert (np.abs(lse - ref_lse) <= (64 + np.array(lens))[:, None] * 2.0 ** -24 * 2).all()
