@@ -50,8 +50,9 @@ constexpr int MANY_ROWS = 1024;
 // places 7 us and 12, 16 of up to 1000 places 15.4 and 18.1, 512 of up to 700 131 and 140; 256 of up to 2000 are better shared,
 // 171 against 186).
 constexpr int TINY_PLACES = 128, SMALL_PLACES = 1024;
-// How far a score may pass the running maximum, as a power of two, before the maximum moves; weights are scaled down by as much.
+// How far a score may pass the running maximum before the maximum moves (a little less than 8 log 2); weights are scaled down by 2^8.
 constexpr int LAG_BITS = 8;
+constexpr float LAG = 5.5f;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 // Rows of places that are not there and dimensions beyond head_dim are read from here: no load leaves the caller's rows, and what
@@ -188,6 +189,9 @@ __device__ __forceinline__ Deal deal(const DecodeArgs& a, int tile) {
   return p;
 }
 
+// exp(x), the last step a power of two
+__device__ __forceinline__ float power(float x) { return __builtin_amdgcn_exp2f(x * LOG2E); }
+
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const bf16x2 v = {(__bf16)lo, (__bf16)hi};
   return __builtin_bit_cast(uint32_t, v);
@@ -236,7 +240,7 @@ __device__ __forceinline__ void store_row(const DecodeArgs& a, int b, int h, int
   char* p = a.out + (int64_t)b * a.o_token + (int64_t)h * a.o_head + d * sizeof(X);
   if constexpr (sizeof(X) == 2) *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
   else *reinterpret_cast<f32x4*>(p) = y;
-  if (a.lse && d == 0) a.lse[(int64_t)b * a.hq + h] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum * (1 << LAG_BITS))) * LN2;
+  if (a.lse && d == 0) a.lse[(int64_t)b * a.hq + h] = sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum * (1 << LAG_BITS)) * LN2;
 }
 
 // A part of the batch per workgroup, piece after piece; its wavefronts take an item's tiles in turn.  An item is a kv head and up to 16
@@ -268,7 +272,6 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) voi
   const char* base = (lane < 32 ? a.k : a.v) + hk * a.head_stride;  // lanes 0-31 place the keys' rows, the others the values'
   const int tp = lane & (TILE - 1);
   const bool plain = a.cap == 0.f && !a.slopes;
-  const float scale2 = a.scale * LOG2E;
   const float slope = a.slopes && m16 < my_heads ? a.slopes[hk * a.G + ht * HEADS + m16] : 0.f;
 
   for (int piece_no = 0; x < x_end; ++piece_no) {
@@ -392,10 +395,10 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) voi
         kept = place_rows(t + step, entry);
         entry = entry_next;
         load_keys();
-        // scores in units of log 2
+        // Scores stay in their own units until the maximum is taken off: in powers of two those beyond 2.4e38 would be infinite.
         if (plain) {
 #pragma unroll
-          for (int st = 0; st < SUB; ++st) z[st] *= scale2;
+          for (int st = 0; st < SUB; ++st) z[st] *= a.scale;
         } else {
 #pragma unroll
           for (int st = 0; st < SUB; ++st)
@@ -404,7 +407,7 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) voi
               float s = z[st][i] * a.scale;
               if (a.cap > 0.f) s = a.cap * tanhf(s * a.inv_cap);
               s -= slope * (float)(n - 1 - (t * TILE + st * 16 + g * 4 + i));
-              z[st][i] = s * LOG2E;
+              z[st][i] = s;
             }
         }
         if (here != EVERY) {
@@ -419,13 +422,13 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) voi
         for (int st = 0; st < SUB; ++st)
 #pragma unroll
           for (int i = 0; i < 4; ++i) top = fmaxf(top, z[st][i]);
-        // The maximum moves only when some score passes it by a factor of 2^8, so that the four lanes of a head need not exchange
+        // The maximum moves only when some score passes it by a factor of nearly 2^8, so that the four lanes of a head need not exchange
         // theirs.  All weights are 2^-8 of what they would be (sums, and so lse, with them): none is above 1, and no product with a
         // finite value overflows.
-        if (__any(top > m + (float)LAG_BITS)) {
+        if (__any(top > m + LAG)) {
           top = fmaxf(top, __shfl_xor(top, 16, 64));
           top = fmaxf(top, __shfl_xor(top, 32, 64));
-          const float now = fmaxf(m, top), f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - now);
+          const float now = fmaxf(m, top), f = now == -INFINITY ? 1.f : power(m - now);
           m = now;
           mref = now == -INFINITY ? 0.f : now;
           l *= f;
@@ -438,7 +441,7 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) voi
         for (int st = 0; st < SUB; ++st)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            z[st][i] = __builtin_amdgcn_exp2f(z[st][i] - mref) * (1.f / (1 << LAG_BITS));
+            z[st][i] = power(z[st][i] - mref) * (1.f / (1 << LAG_BITS));
             l += z[st][i];
           }
         if constexpr (BF16) {
@@ -493,7 +496,7 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X))) voi
       for (w &= wave_heads - 1; w < WAVES; w += wave_heads) top = fmaxf(top, ml_lds[w][row][0]);
       return top;
     };
-    auto part_weight = [&](int w, int row, float top) { return top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml_lds[w][row][0] - top); };
+    auto part_weight = [&](int w, int row, float top) { return top == -INFINITY ? 1.f : power(ml_lds[w][row][0] - top); };
     const float f = m16 < my_heads ? part_weight(wave, m16, joined_max(wave, m16)) : 0.f;
     const int d = threadIdx.x % (BD / 4) * 4;
 #pragma unroll
@@ -587,7 +590,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(DecodeArgs a) {
   float sum = 0.f;
   for (int j = tid; j < plan.y; j += ROW) {
     const f32x2 ml = a.part_ml[row(j)];
-    const float f = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[0] - top);
+    const float f = top == -INFINITY ? 1.f : power(ml[0] - top);
     weight[j] = f;
     sum += f * ml[1];
   }

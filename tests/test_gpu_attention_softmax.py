@@ -60,3 +60,25 @@ def test_large_values_under_rising_scores(dtype, D, far):
     tol = (64 + np.array(lens))[:, None, None] * 2.0 ** -24 * mean_abs + HALF_STEP[dtype] * 1.01 * np.abs(ref)
     assert (np.abs(out - ref) <= tol).all()
     assert (np.abs(lse - ref_lse) <= (64 + np.array(lens))[:, None] * 2.0 ** -24 * 2).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("sign", [-1.0, 1.0])
+def test_scores_near_the_largest_number(sign, dtype):
+    """Scores of 3e38 either way are numbers, not infinities: equal ones share the weight, the mean of n values is off by (n + 8)
+    float32 roundings of the mean of |v| and one of its own.  lse is the score, to a rounding."""
+    lens = [1, 40, 300, 2500]
+    p = Paged(lens, 2, 64, 16, dtype)
+    big = torch.tensor(sign * 3e38).to(DT[dtype]).item()
+    held = ~np.isnan(p.k)
+    p.k[held] = 0.0
+    p.k[..., 0] = np.where(held[..., 0], big, np.nan)
+    q = torch.zeros(4, 4, 64)
+    q[:, :, 0] = 1.0
+    for kw in (dict(scale=1.0), dict(scale=1.0, window=17)):
+        out, lse = attend(p.cache(), q.to(DT[dtype]), p.lens, **kw)
+        ref, ref_lse, mean_abs, *_ = A.decode(p.k, p.v, p.table, q.numpy(), p.lens, **kw)
+        tol = (np.array(lens) + 8)[:, None, None] * 2.0 ** -24 * mean_abs + HALF_STEP[dtype] * 1.01 * np.abs(ref)
+        off = ~(np.abs(out - ref) <= tol)
+        assert not off.any(), f"{off.sum()} of {off.size} off: {out[off][:4]} for {ref[off][:4]}"
+        assert (np.abs(lse / ref_lse - 1.0) <= 2.0 ** -23).all()
