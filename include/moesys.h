@@ -563,7 +563,8 @@ typedef struct {
  * way, which is the gradient as well: with d_out for x it gives d_x.  The angle is taken in float64 and reduced to
  * one turn (positions of any size keep their angle), cosine, sine and rotation are float32, rounded once to dtype.
  * x, out [T, n_heads, head_dim] of dtype (moe_dtype); out may be x itself (same data and strides), and must not
- * overlap it otherwise.  positions device int32 [n_axes, T], any sign. */
+ * overlap it otherwise.  positions device int32 [n_axes, T], any sign.  MOE_ERR_UNSUPPORTED beyond 2^26 - 4 tokens (what one
+ * launch holds), here and in moe_kv_append. */
 int32_t moe_rotary(const moe_rotary_spec* r, int32_t dtype, int32_t T, int32_t n_heads, const moe_head_rows* x,
                    const int32_t* positions, const moe_head_rows* out, int32_t inverse, void* stream);
 
@@ -618,7 +619,9 @@ typedef struct {
  * Products of MOE_BF16 are exact and accumulated in float32, softmax weights are float32 numbers with all their bits,
  * out is rounded once.
  * q, out [n_seqs, n_q_heads, head_dim], pointers and strides multiples of 16 bytes; n_q_heads a multiple of
- * n_kv_heads; lse (nullable) device float [n_seqs, n_q_heads].  ws: moe_attention_decode_workspace_bytes, 256-byte
+ * n_kv_heads; lse (nullable) device float [n_seqs, n_q_heads].  MOE_ERR_UNSUPPORTED, before any launch, where there are more
+ * sequences than a launch holds: n_seqs*n_q_heads beyond 2^26 - 4, or, where the table or the window keeps sequences short, 2^24
+ * workgroups of one to four kv heads each.  ws: moe_attention_decode_workspace_bytes, 256-byte
  * aligned, need not be cleared, one call at a time.  Results do not depend on what else runs: the split over the
  * length follows from the lengths alone, and its parts are joined in order. */
 size_t moe_attention_decode_workspace_bytes(const moe_kv_cache* c, int32_t n_q_heads);

@@ -615,7 +615,8 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(DecodeArgs a) {
 
 // The split of a call: what its grid, its workspace and its kernels agree on.
 struct Split {
-  int rows, items, wave_heads, least, grid, parts;
+  int rows, items, wave_heads, least, parts;
+  int64_t grid;  // workgroups of the decode kernel
   bool nt, join;
   size_t ml, o, total;  // bytes: offsets of the pieces (the plan lies in front)
 };
@@ -638,7 +639,7 @@ Split split_of(const moe_kv_cache* c, int32_t n_q_heads, int32_t window) {
   int64_t grid = (int64_t)c->n_seqs * s.items * (pieces > 1 ? pieces : 1);
   if (grid > resident) grid = resident;
   if (grid < s.items) grid = s.items;
-  s.grid = (int)grid;
+  s.grid = grid;
   s.parts = (int)(grid * (s.items % 4 == 0 ? 4 : s.items % 2 == 0 ? 2 : 1) / s.items);  // the most there can be
   // sequences that no deal splits: no second launch, and no look at all the lengths
   const int64_t kept = window > 0 && window + tile < capacity ? window + tile : capacity;
@@ -647,7 +648,7 @@ Split split_of(const moe_kv_cache* c, int32_t n_q_heads, int32_t window) {
   if (!s.join && work > grid) {
     // more short sequences than one round holds: a workgroup for each, so that the long ones among them do not meet
     const int wave_heads = kept > TINY_PLACES ? s.wave_heads : s.items % 4 == 0 ? 4 : s.items % 2 == 0 ? 2 : 1;
-    s.grid = (int)(work / wave_heads);
+    s.grid = work / wave_heads;
   }
   // Pools that the last-level cache (256 MB) cannot keep for the next call are read past it: 537 MB 99 us, 107 through the caches; of
   // 79 MB that it keeps 27 and 24.
@@ -657,6 +658,9 @@ Split split_of(const moe_kv_cache* c, int32_t n_q_heads, int32_t window) {
   s.total = s.o + align_up((size_t)s.parts * 2 * s.items * s.rows * c->head_dim * sizeof(float), 256);
   return s;
 }
+
+// Workgroups of the join of so many rows: four rows each where there are many.
+int64_t join_grid(int64_t rows) { return rows >= MANY_ROWS ? (rows * 64 + JOIN_THREADS - 1) / JOIN_THREADS : rows; }
 
 template <typename X, int DP, bool NT>
 void launch(const DecodeArgs& a, unsigned grid, hipStream_t s) {
@@ -680,12 +684,13 @@ int32_t launch_decode(const DecodeArgs& a, const Split& sp, hipStream_t s) {
   int32_t st = check_hip(hipGetLastError(), "attention launch");
   if (st != MOE_OK || !sp.join) return st;
   const int64_t rows = (int64_t)a.n_seqs * a.hq;
+  const unsigned join = (unsigned)join_grid(rows);
   // (a row has about parts / sequences pieces; the weights of four rows' take LDS)
   if (rows >= MANY_ROWS) {
     const size_t lds = (size_t)sp.parts * (JOIN_THREADS / 64) * sizeof(float);
-    hipLaunchKernelGGL((join_kernel<X, 64>), dim3((unsigned)((rows * 64 + JOIN_THREADS - 1) / JOIN_THREADS)), dim3(JOIN_THREADS), lds, s, a);
+    hipLaunchKernelGGL((join_kernel<X, 64>), dim3(join), dim3(JOIN_THREADS), lds, s, a);
   } else {
-    hipLaunchKernelGGL((join_kernel<X, JOIN_THREADS>), dim3((unsigned)rows), dim3(JOIN_THREADS), (size_t)sp.parts * sizeof(float), s, a);
+    hipLaunchKernelGGL((join_kernel<X, JOIN_THREADS>), dim3(join), dim3(JOIN_THREADS), (size_t)sp.parts * sizeof(float), s, a);
   }
   return check_hip(hipGetLastError(), "attention join launch");
 }
@@ -721,7 +726,8 @@ extern "C" int32_t moe_attention_decode(const moe_kv_cache* c, int32_t n_q_heads
   if (!rows_aligned(q, es) || !rows_aligned(out, es))
     return fail(MOE_ERR_INVALID_ARG, "moe_attention_decode: pointers and strides of q and out must be multiples of 16 bytes");
   const Split sp = split_of(c, n_q_heads, opt->window);
-  if ((int64_t)c->n_seqs * n_q_heads > INT32_MAX)
+  // (a sequence has at most 64 query heads per workgroup: their product stays below 2^31)
+  if (!launchable(sp.grid, 64 * WAVES) || (sp.join && !launchable(join_grid((int64_t)c->n_seqs * n_q_heads), JOIN_THREADS)))
     return fail(MOE_ERR_UNSUPPORTED, "moe_attention_decode: %d sequences of %d query heads are too many for one call", c->n_seqs, n_q_heads);
   if (!ws || ((uintptr_t)ws & 255) || ws_bytes < need)
     return fail(MOE_ERR_WORKSPACE, "moe_attention_decode: workspace NULL, misaligned or smaller than %zu bytes", need);
@@ -758,7 +764,7 @@ extern "C" int32_t moe_attention_decode(const moe_kv_cache* c, int32_t n_q_heads
     const int groups = sp.items >> k;
     if (groups == 0) continue;  // (never taken)
     a.share_of_grid[k].per_part = page_divisor(groups);
-    a.share_of_grid[k].parts = sp.grid / groups;
+    a.share_of_grid[k].parts = (int)(sp.grid / groups);
     a.share_of_grid[k].inverse_parts = 1.0 / a.share_of_grid[k].parts;
   }
   a.hts = sp.items / c->n_kv_heads;

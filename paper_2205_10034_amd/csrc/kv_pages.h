@@ -34,6 +34,9 @@ inline PageDivisor page_divisor(int d) {
   return PageDivisor{(uint32_t)(((1ull << (31 + s)) + (uint64_t)d - 1) / (uint64_t)d), 31 + s};
 }
 
+// A launch holds fewer than 2^32 work-items: more are refused before anything of the call runs.
+inline bool launchable(int64_t workgroups, int threads) { return workgroups < (1ll << 32) / threads; }
+
 // How attention deals the batch out.  The sequences' tiles stand in one row, sequence after sequence, an empty one as one tile
 // (somebody has to write its zeros); part w of the row is the tiles w*share .. (w+1)*share - 1.  A part holds pieces of one or more
 // sequences; a sequence that lies in one part is finished there, the pieces of the others are joined.

@@ -225,7 +225,7 @@ int32_t launch_tokens(TokenArgs& a, const moe_rotary_spec* r, int32_t dtype, hip
   const int64_t trips = (a.units + 63) / 64, wanted = (ENOUGH_WAVES + a.T - 1) / a.T;
   a.splits = (int)(wanted < trips ? wanted : trips);
   const int64_t grid = ((int64_t)a.T * a.splits + WAVES - 1) / WAVES;
-  if (grid > INT32_MAX) return fail(MOE_ERR_UNSUPPORTED, "%d tokens are too many for one call", a.T);
+  if (!launchable(grid, 64 * WAVES)) return fail(MOE_ERR_UNSUPPORTED, "%d tokens are too many for one call", a.T);
   if (dtype == MOE_BF16) {
     if (bytes == 16) launch_of<__bf16, 16>(a, (unsigned)grid, interleaved, s);
     else if (bytes == 8) launch_of<__bf16, 8>(a, (unsigned)grid, interleaved, s);
