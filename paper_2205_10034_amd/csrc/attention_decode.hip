@@ -651,8 +651,11 @@ Split split_of(const moe_kv_cache* c, int32_t n_q_heads, int32_t window) {
     s.grid = work / wave_heads;
   }
   // Pools that the last-level cache (256 MB) cannot keep for the next call are read past it: 537 MB 99 us, 107 through the caches; of
-  // 79 MB that it keeps 27 and 24.
-  s.nt = (double)c->n_pages * c->page_size * c->n_kv_heads * c->head_dim * 2 * es > (double)(300 << 20);
+  // 79 MB that it keeps 27 and 24.  The pool's size counts and not what a call reads of it: of a pool of 3 GB, other places in each call,
+  // 135 MB 33.6 us and 37.5, 25 MB 15.3 and 16.1, 0.7 MB 7.4 and 7.5 (the same places again and again 32.0 and 30.3, 14.5 and 14.3, 7.4 and
+  // 7.5).  Not where tiles of query heads read the same keys and values one beside the other: 64 heads on one kv head, 153 MB, 78 us
+  // and 70, 32 on each of four, 307 MB, 93 and 86.
+  s.nt = !several && (double)c->n_pages * c->page_size * c->n_kv_heads * c->head_dim * 2 * es > (double)(300 << 20);
   s.ml = align_up((size_t)c->n_seqs * sizeof(int2), 256);
   s.o = s.ml + align_up((size_t)s.parts * 2 * s.items * s.rows * sizeof(f32x2), 256);
   s.total = s.o + align_up((size_t)s.parts * 2 * s.items * s.rows * c->head_dim * sizeof(float), 256);
