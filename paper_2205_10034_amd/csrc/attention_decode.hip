@@ -25,6 +25,8 @@
 // four dependent trips to memory.
 #include "attention_internal.h"
 #include "wave_util.h"
+#include <float.h>
+#include <math.h>
 
 namespace moesys {
 namespace {
@@ -781,6 +783,7 @@ extern "C" int32_t moe_attention_decode(const moe_kv_cache* c, int32_t n_q_heads
   a.may_split = sp.join;
   a.scale = opt->scale;
   a.cap = opt->softcap;
-  a.inv_cap = opt->softcap > 0.f ? 1.f / opt->softcap : 0.f;
+  // (finite for the smallest caps too: a score of 0 stays 0)
+  a.inv_cap = opt->softcap > 0.f ? fminf(1.f / opt->softcap, FLT_MAX) : 0.f;
   return c->dtype == MOE_BF16 ? launch_decode<__bf16>(a, sp, (hipStream_t)stream) : launch_decode<float>(a, sp, (hipStream_t)stream);
 }

@@ -82,3 +82,19 @@ def test_scores_near_the_largest_number(sign, dtype):
         off = ~(np.abs(out - ref) <= tol)
         assert not off.any(), f"{off.sum()} of {off.size} off: {out[off][:4]} for {ref[off][:4]}"
         assert (np.abs(lse / ref_lse - 1.0) <= 2.0 ** -23).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_smallest_caps(dtype):
+    """A cap whose reciprocal float32 does not hold leaves scores of nearly nothing: all places weigh the same, 0 scores included."""
+    lens = [3, 70]
+    p = Paged(lens, 1, 64, 16, dtype)
+    q = torch.zeros(2, 2, 64)
+    q[:, 1] = 3.0
+    for cap in (1e-45, 1e-39, 1.2e-38, 1e-30):
+        out, lse = attend(p.cache(), q.to(DT[dtype]), p.lens, softcap=cap)
+        ref, ref_lse, mean_abs, *_ = A.decode(p.k, p.v, p.table, q.numpy(), p.lens, 0.125, softcap=cap)
+        tol = (np.array(lens) + 8)[:, None, None] * 2.0 ** -24 * mean_abs + HALF_STEP[dtype] * 1.01 * np.abs(ref)
+        off = int((~(np.abs(out - ref) <= tol)).sum())
+        assert off == 0, f"cap {cap}: {off} of {out.size} off"
+        assert np.abs(lse - ref_lse).max() <= 8 * 2.0 ** -24 * 5
