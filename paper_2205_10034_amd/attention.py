@@ -15,6 +15,7 @@ import torch
 from . import binding as B
 
 _MAX_AXES = 3
+_MAX_INT = 2 ** 31 - 1
 
 
 class _HeadRows(C.Structure):
@@ -55,6 +56,19 @@ def lib() -> C.CDLL:
         L.moe_attention_decode.argtypes = [C.POINTER(_Cache), C.c_int32, rows, vp, C.POINTER(_Options), rows, vp, vp, C.c_size_t, vp]
         _lib = L
     return _lib
+
+
+def _int32(n: int, what: str) -> int:
+    """A number that the library takes as int32 (ctypes would cut it down to 32 bits)."""
+    if not -_MAX_INT - 1 <= n <= _MAX_INT:
+        raise ValueError(f"{what}={n} is beyond int32")
+    return n
+
+
+def _options(scale: float, softcap: float, window: int, slopes: Optional[int]) -> _Options:
+    if not -1 <= window <= _MAX_INT:
+        window = -1 if window < 0 else _MAX_INT  # (no sequence is longer)
+    return _Options(scale, softcap, window, slopes)
 
 
 def _dtype(t) -> int:
@@ -113,11 +127,11 @@ class Rotary:
         if freqs.dtype != torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous():
             raise ValueError("freqs must be a contiguous float64 vector")
         self.device = _device(freqs, "freqs")
-        pairs = [freqs.numel()] if axis_pairs is None else [int(n) for n in axis_pairs]
+        pairs = [freqs.numel()] if axis_pairs is None else [_int32(int(n), "axis_pairs") for n in axis_pairs]
         if not 1 <= len(pairs) <= _MAX_AXES:
             raise ValueError(f"{len(pairs)} axes: 1 to {_MAX_AXES} are supported")
         self.freqs, self.head_dim, self.n_axes = freqs, head_dim, len(pairs)
-        self.c = _RotarySpec(head_dim, 2 * freqs.numel(), int(bool(interleaved)), len(pairs),
+        self.c = _RotarySpec(_int32(head_dim, "head_dim"), _int32(2 * freqs.numel(), "rot_dim"), int(bool(interleaved)), len(pairs),
                              (C.c_int32 * _MAX_AXES)(*(pairs + [0] * (_MAX_AXES - len(pairs)))), freqs.data_ptr())
 
 
@@ -150,6 +164,8 @@ class KVCache:
         tok, head = (1, 2) if layout == "token_major" else (2, 1)
         self.page_size, self.n_kv_heads, self.head_dim = k.shape[tok], k.shape[head], k.shape[3]
         self.n_seqs, self.dtype = page_table.shape[0], k.dtype
+        for n in tuple(k.shape[1:]) + tuple(page_table.shape):
+            _int32(n, "a dimension of the cache")
         self.scale = self.head_dim ** -0.5
         self.c = _Cache(k.data_ptr() or None, v.data_ptr() or None, page_table.data_ptr() or None, k.shape[0], k.stride(0), k.stride(tok),
                         k.stride(head), self.page_size, page_table.shape[0], page_table.shape[1], self.n_kv_heads, self.head_dim, _dtype(k))
@@ -160,6 +176,8 @@ def moe_rotary(rotary: Rotary, x, positions, out, inverse: bool = False, stream=
     """out <- x [T, heads, head_dim] rotated by positions [axes, T] (int32; [T] for one axis); ``inverse``: back, or the gradient."""
     shape, dtype, device = tuple(x.shape), x.dtype, rotary.device
     T, H, D = shape
+    if T > _MAX_INT or H > _MAX_INT:
+        _int32(max(T, H), "tokens or heads")
     if D != rotary.head_dim:
         raise ValueError(f"x has heads of {D}, the rotary positions are for {rotary.head_dim}")
     st = lib().moe_rotary(rotary.c, _dtype(x), T, H, _rows(x, "x", shape, dtype, device), _positions(rotary, positions, T, device),
@@ -178,6 +196,8 @@ def moe_kv_append(cache: KVCache, k, v, cache_pos, token_seq=None, rotary: Optio
     """Keys and values [T, kv_heads, head_dim] of new tokens into their places of the cache, keys rotated; queries
     [T, heads, head_dim] rotated into q_out."""
     T, D, dtype, device = k.shape[0], cache.head_dim, cache.dtype, cache.device
+    if T > _MAX_INT:
+        _int32(T, "tokens")
     shape, per_token = (T, cache.n_kv_heads, D), (T,)
     spec = pos = q_rows = q_out_rows = None
     heads = 0
@@ -193,6 +213,8 @@ def moe_kv_append(cache: KVCache, k, v, cache_pos, token_seq=None, rotary: Optio
         if q_out is None:
             raise ValueError("q without q_out")
         heads = q.shape[1]
+        if heads > _MAX_INT:
+            _int32(heads, "heads")
         q_shape = (T, heads, D)
         q_rows, q_out_rows = _rows(q, "q", q_shape, dtype, device), _rows(q_out, "q_out", q_shape, dtype, device)
     st = lib().moe_kv_append(cache.c, T, _rows(k, "k", shape, dtype, device), _rows(v, "v", shape, dtype, device),
@@ -203,7 +225,7 @@ def moe_kv_append(cache: KVCache, k, v, cache_pos, token_seq=None, rotary: Optio
 
 
 def moe_attention_decode_workspace_bytes(cache: KVCache, n_q_heads: int) -> int:
-    n = lib().moe_attention_decode_workspace_bytes(cache.c, n_q_heads)
+    n = lib().moe_attention_decode_workspace_bytes(cache.c, _int32(n_q_heads, "n_q_heads"))
     if n == 0:
         raise B.MoEError(1, "moe_attention_decode_workspace_bytes", lib().moe_last_error().decode())
     return n
@@ -214,10 +236,12 @@ def moe_attention_decode(cache: KVCache, q, seq_lens, out, ws, scale: Optional[f
     """Attention of one new token per sequence: q, out [sequences, heads, head_dim], seq_lens int32 [sequences] (the new token
     counted), slopes float32 [heads] (optional), lse float32 [sequences, heads] (optional output)."""
     S, H, dtype, device = cache.n_seqs, q.shape[1], cache.dtype, cache.device
+    if H > _MAX_INT:
+        _int32(H, "heads")
     shape = (S, H, cache.head_dim)
     if not ws.is_contiguous() or ws.get_device() != device:
         raise ValueError("the workspace must be contiguous and on the cache's device")
-    options = _Options(cache.scale if scale is None else scale, softcap, window, _vector(slopes, "slopes", torch.float32, (H,), device))
+    options = _options(cache.scale if scale is None else scale, softcap, window, _vector(slopes, "slopes", torch.float32, (H,), device))
     st = lib().moe_attention_decode(cache.c, H, _rows(q, "q", shape, dtype, device), _vector(seq_lens, "seq_lens", torch.int32, (S,), device), options,
                                     _rows(out, "out", shape, dtype, device), _vector(lse, "lse", torch.float32, (S, H), device),
                                     ws.data_ptr(), ws.nbytes, _stream(stream, device))

@@ -2,7 +2,9 @@
 import ctypes as C
 
 import pytest
+import torch
 
+import paper_2205_10034_amd as M
 from paper_2205_10034_amd import attention as B
 from test_attention_abi import FAKE, OPT, ROWS, cache, compiled, rotary
 
@@ -38,3 +40,25 @@ def test_what_a_launch_can_do_on_the_host(tmp_path):
   assert(launchable(1, 256) && launchable((1 << 24) - 1, 256) && !launchable(1 << 24, 256) && !launchable(1ll << 40, 256));
   assert(launchable(4294967295ll, 1) && !launchable(4294967296ll, 1) && !launchable(1ll << 31, 256));
 }""")
+
+
+def test_numbers_beyond_32_bits_are_not_cut():
+    """What the library takes as int32 is refused by the binding, or kept in meaning, and never loses its upper bits."""
+    meta = lambda *shape, dtype=torch.bfloat16: torch.empty(*shape, dtype=dtype, device="meta")
+    assert B._int32(2 ** 31 - 1, "n") == 2 ** 31 - 1 and B._int32(-3, "n") == -3
+    for n in (2 ** 31, 2 ** 32 + 1, -2 ** 31 - 1):
+        with pytest.raises(ValueError, match="int32"):
+            B._int32(n, "n")
+    # a window longer than any sequence is no window; a negative one stays what the library refuses
+    for window, taken in ((0, 0), (5, 5), (2 ** 31 - 1, 2 ** 31 - 1), (2 ** 32 + 1, 2 ** 31 - 1), (2 ** 63 - 1, 2 ** 31 - 1), (-1, -1), (-2 ** 32 + 7, -1)):
+        assert B._options(0.5, 1.5, window, None).window == taken
+    x = meta(2 ** 32 + 1, 1, 2)
+    rot = type("R", (), dict(device=-1, head_dim=2, n_axes=1, c=rotary(head_dim=2, rot_dim=2, pairs=(1,))))
+    with pytest.raises(ValueError, match="int32"):
+        M.moe_rotary(rot, x, meta(1, 2 ** 32 + 1, dtype=torch.int32), x)
+    pool = type("P", (), dict(device=-1, dtype=torch.bfloat16, head_dim=64, n_kv_heads=1, n_seqs=1, c=cache()))
+    with pytest.raises(ValueError, match="int32"):
+        k = meta(2 ** 32 + 1, 1, 64)
+        M.moe_kv_append(pool, k, k, meta(2 ** 32 + 1, dtype=torch.int32))
+    with pytest.raises(ValueError, match="int32"):
+        M.moe_attention_decode_workspace_bytes(pool, 2 ** 32 + 4)
