@@ -623,7 +623,8 @@ typedef struct {
  * sequences than a launch holds: n_seqs*n_q_heads beyond 2^26 - 4, or, where the table or the window keeps sequences short, 2^24
  * workgroups of one to four kv heads each.  ws: moe_attention_decode_workspace_bytes, 256-byte
  * aligned, need not be cleared, one call at a time.  Results do not depend on what else runs: the split over the
- * length follows from the lengths alone, and its parts are joined in order. */
+ * length follows from the lengths, the window and the cache's shape (sequences, heads, table width, page size, strides),
+ * and its parts are joined in order.  Equal lengths under a wider table may be split otherwise, and round otherwise. */
 size_t moe_attention_decode_workspace_bytes(const moe_kv_cache* c, int32_t n_q_heads);
 int32_t moe_attention_decode(const moe_kv_cache* c, int32_t n_q_heads, const moe_head_rows* q, const int32_t* seq_lens,
                              const moe_attention_options* opt, const moe_head_rows* out, float* lse, void* ws,

@@ -20,9 +20,9 @@
 //    flight while the other is used, and the other wavefronts of the CU hide the rest.
 //  - All sequences' tiles stand in one row that the resident workgroups share evenly (Deal): no last round, no long sequence that
 //    the others wait for.
-// Measured: 256 sequences of 2048 to 14336 places, 64 query and 8 kv heads of 128 (8.5 GB of keys and values) 1253 us, 6.8 TB/s; 64 of
-// 100 to 8192 (1.3 GB) 200 us, 6.5 TB/s; one of 131071 (0.54 GB) 89 us, of which the join takes 5; one of 173, 16 heads of 64: 7 us,
-// four dependent trips to memory.
+// Measured: 256 sequences of 2048 to 14336 places, 64 query and 8 kv heads of 128 (8.5 GB of keys and values) 1262 us, 6.7 TB/s; 64 of
+// 100 to 8192 (1.3 GB) 201 us, 6.5 TB/s; one of 131071 (0.54 GB) 88 us, of which the join takes 5; one of 173, 16 heads of 64: 7 us,
+// four dependent trips to memory, and 10 with a page table of 1000 more columns, which alone decide whether the join is launched.
 #include "attention_internal.h"
 #include "wave_util.h"
 #include <float.h>
@@ -41,16 +41,17 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int WAVES = 4;
 constexpr int HEADS = 16;  // query heads of a tile
-// Tiles of a part for each of its wavefronts, at least: 8 sequences of 100 to 1500 places take 17.2 us with 2, 18.4 with 1 and 19.4
-// with 4 (more pieces to join, fewer CUs at work).
+// Tiles of a part for each of its wavefronts, at least: 8 sequences of 100 to 1500 places take 15.9 us with 2 or 1 and 16.8 with 4, 150 of
+// up to 300 31.6, 31.7 and 33.9 (fewer CUs at work).
 constexpr int LEAST_PER_WAVE = 2;
-// Joins of so many rows take a wavefront each: 16384 rows of 2 to 3 pieces 6.5 us, 12.2 with a workgroup each.
+// Joins of so many rows take a wavefront each: of 16384 rows, with the attention before them, 1261 us, 1269 with a workgroup each; of 8192
+// 172 and 178.
 constexpr int MANY_ROWS = 1024;
 // Sequences that are not split.  None longer than TINY_PLACES: a piece's four trips to memory are all there is, so the fewest rounds
-// of workgroups count (292 sequences of one place, 16 heads of 192: 24 us; shared evenly, 9 pieces one after the other per
-// workgroup, 68).  None longer than SMALL_PLACES, and a workgroup for each: the join would cost more than it saves (one of 173
-// places 7 us and 12, 16 of up to 1000 places 15.4 and 18.1, 512 of up to 700 131 and 140; 256 of up to 2000 are better shared,
-// 171 against 186).
+// of workgroups count (292 sequences of one place, 16 heads of 192: 19 us; shared evenly, 9 pieces one after the other per
+// workgroup, 36).  None longer than SMALL_PLACES, and a workgroup for each: the join would cost more than it saves (one of 173
+// places 7.7 us and 12.2, 16 of up to 1000 places 15.5 and 18.3, 512 of up to 700 128 and 144; 256 of up to 2000 are better shared,
+// 172 against 197).
 constexpr int TINY_PLACES = 128, SMALL_PLACES = 1024;
 // How far a score may pass the running maximum before the maximum moves (a little less than 8 log 2); weights are scaled down by 2^8.
 constexpr int LAG_BITS = 8;
@@ -61,9 +62,10 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 // lies in places that are not kept reaches no product.
 __device__ const u32x4 ZEROS[MOE_MAX_HEAD_DIM * 4 / 16] = {};
 
-// Workgroups of the decode kernel that a CU holds: two need up to 256 registers a lane, which keys and values of 128 dimensions on
-// their way leave room for; a third or a fourth costs registers for what is in flight (64 sequences, 1.3 GB: 210 us with two,
-// 237 with three), and 256 dimensions need more than 256 (130 MB: 48 us with one, 64 with two, which spill).
+// Workgroups of the decode kernel that a CU holds: two need up to 256 registers a lane, which keys and values on their way leave room
+// for; a third or a fourth costs registers for what is in flight (64 sequences, 1.3 GB: 210 us with two, 237 with three).  256 dimensions
+// of float32 need more than 256 (0.5 GB: 100 us with one, 163 with two, which spill); of bfloat16, in tiles of 16 places, they do not
+// (96 sequences with a window 44.3 us with two, 44.7 with one).
 constexpr int resident_workgroups(int dims, int elem) { return dims <= 128 || elem == 2 ? 2 : 1; }
 
 struct DecodeArgs {
@@ -628,9 +630,9 @@ Split split_of(const moe_kv_cache* c, int32_t n_q_heads, int32_t window) {
   const int G = n_q_heads / c->n_kv_heads, es = (int)elem_size(c->dtype), tile = es == 2 && c->head_dim <= 128 ? 32 : 16;
   s.rows = G < HEADS ? G : HEADS;
   s.items = c->n_kv_heads * ((G + HEADS - 1) / HEADS);
-  // Neighbouring items by one workgroup: tiles of query heads that read the same keys and values (64 heads on one kv head 104 us
-  // apart, 83 together), and kv heads whose rows are neighbours in memory, 512 bytes of them (256-byte rows, 8.5 GB: 1334 us one by
-  // one, 1263 by twos, 1308 by fours; 128-byte rows: 107, 100 and 93).
+  // Neighbouring items by one workgroup: tiles of query heads that read the same keys and values (64 heads on one kv head 97 us
+  // apart, 73 together), and kv heads whose rows are neighbours in memory, 512 bytes of them (256-byte rows, 8.5 GB: 1333 us one by
+  // one, 1261 by twos, 1308 by fours; 128-byte rows: 108, 96 and 90).
   const bool several = s.items > c->n_kv_heads, neighbours = c->head_stride < c->token_stride;
   const int wanted = several ? 4 : !neighbours ? 1 : c->head_dim * es <= 128 ? 4 : 2;
   s.wave_heads = s.items % wanted == 0 ? wanted : s.items % 2 == 0 && wanted > 1 ? 2 : 1;
@@ -652,8 +654,8 @@ Split split_of(const moe_kv_cache* c, int32_t n_q_heads, int32_t window) {
     const int wave_heads = kept > TINY_PLACES ? s.wave_heads : s.items % 4 == 0 ? 4 : s.items % 2 == 0 ? 2 : 1;
     s.grid = work / wave_heads;
   }
-  // Pools that the last-level cache (256 MB) cannot keep for the next call are read past it: 537 MB 99 us, 107 through the caches; of
-  // 79 MB that it keeps 27 and 24.  The pool's size counts and not what a call reads of it: of a pool of 3 GB, other places in each call,
+  // Pools that the last-level cache (256 MB) cannot keep for the next call are read past it: 537 MB 89 us, 101 through the caches; of
+  // 79 MB that it keeps 25.9 and 25.2.  The pool's size counts and not what a call reads of it: of a pool of 3 GB, other places in each call,
   // 135 MB 33.6 us and 37.5, 25 MB 15.3 and 16.1, 0.7 MB 7.4 and 7.5 (the same places again and again 32.0 and 30.3, 14.5 and 14.3, 7.4 and
   // 7.5).  Not where tiles of query heads read the same keys and values one beside the other: 64 heads on one kv head, 153 MB, 78 us
   // and 70, 32 on each of four, 307 MB, 93 and 86.
