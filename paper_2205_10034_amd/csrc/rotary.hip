@@ -138,6 +138,8 @@ __global__ __launch_bounds__(64 * WAVES) void token_kernel(TokenArgs a) {
         // in float64, reduced to one turn: in float32 the angle of position 10^6 would be off by 0.06
         double turns = (double)a.positions[(int64_t)axis * a.T + t] * a.freqs[i] * 0.15915494309189533577;
         turns -= rint(turns);
+        // Cosine and sine themselves in float32, as the rotation is: float32 results are off by 4.1e-8 of their size, and by 3.7e-8 with
+        // both taken in float64, which costs 8192 tokens' rotation 2 % (9.0 us and 8.8).
         const float near = (float)turns, off = 6.2831853f * (float)(turns - near);  // what rounding to float32 took, in radians
         float s, c;
         sincospif(2.0f * near, &s, &c);
