@@ -630,6 +630,106 @@ int32_t moe_attention_decode(const moe_kv_cache* c, int32_t n_q_heads, const moe
                              const moe_attention_options* opt, const moe_head_rows* out, float* lse, void* ws,
                              size_t ws_bytes, void* stream);
 
+/* ---- a step of drafted tokens --------------------------------------------- */
+/*
+ * Several tokens per sequence in one step of the model, guesses of a smaller one as a rule: attention in which each of
+ * them sees the cache and its own ancestors among them, the places of those that were accepted, and the pages of the
+ * cache.  What judges the guesses, moe_token_logprobs, stands behind.  Same rules as above.
+ */
+
+#define MOE_MAX_DRAFTS 64 /* new tokens of a sequence in one call */
+
+typedef struct {
+  float scale;         /* of the scores, usually head_dim^-1/2                                       */
+  float softcap;       /* > 0: scores are capped, softcap*tanh(score/softcap); 0: not                */
+  int32_t window;      /* > 0: a token sees positions less than `window` behind its own; 0: all      */
+  int32_t sinks;       /* with a window: the first `sinks` places of a sequence stay visible         */
+  const float* slopes; /* nullable: device float [n_q_heads], score -= slope*(distance in positions) */
+} moe_tree_options;
+
+/* Attention of the new tokens of every sequence over its cache, which holds their own keys and values already
+ * (moe_kv_append).  T tokens in all; those of sequence s are token_first[s] .. token_first[s+1]-1 (device int32
+ * [n_seqs+1], rising, cut to 0..T and to max_new tokens a sequence, 1..MOE_MAX_DRAFTS), n of them.  Sequence s has
+ * seq_lens[s] places (device int32 [n_seqs], clamped to 0..table_width*page_size), its new tokens' at the end: the i-th
+ * is place base + i, base = max(0, seq_lens[s] - n) (one beyond seq_lens[s] has no key).
+ * visible (device uint64 [T], nullable): token i of its sequence sees token j where bit j of its word is set, its own
+ * key included only if bit i is; bits from n on mean nothing.  NULL: each sees itself and those before it.
+ * Positions: place j < base is at position j, token i at base + (bits of its word other than its own), which in a tree
+ * whose words name all ancestors is its depth.  Token i sees, on pages that are there,
+ *   the places j < base and the tokens of its word, of those the ones at positions > its own - window (window > 0), and
+ *   with a window also those of the places 0..sinks-1.
+ * Scores, sums, out and lse as in moe_attention_decode, with the distance pos_i - pos_j for slopes; a token that sees
+ * nothing has out = 0, lse = -infinity.  For MOE_BF16 a softmax weight enters as two bfloat16 numbers, 17 bits of it.
+ * q, out [T, n_q_heads, head_dim], pointers and strides multiples of 16 bytes; out must not overlap q; lse (nullable)
+ * device float [T, n_q_heads].  Rows of tokens that belong to no sequence are left as they were.  MOE_ERR_UNSUPPORTED
+ * where T*n_q_heads or the work of one launch is beyond 2^26 - 4.  ws: moe_attention_tree_workspace_bytes, 256-byte
+ * aligned, need not be cleared, one call at a time.  Results do not depend on what else runs. */
+size_t moe_attention_tree_workspace_bytes(const moe_kv_cache* c, int32_t n_q_heads, int32_t max_new);
+int32_t moe_attention_tree(const moe_kv_cache* c, int32_t n_q_heads, int32_t T, int32_t max_new, const moe_head_rows* q,
+                           const int32_t* token_first, const int32_t* seq_lens, const uint64_t* visible,
+                           const moe_tree_options* opt, const moe_head_rows* out, float* lse, void* ws, size_t ws_bytes,
+                           void* stream);
+
+/* The accepted ones of a sequence's new tokens move up behind its base: place base[s] + keep[s, i] becomes place
+ * base[s] + i, for i from 0 to the first negative keep[s, i] (device int32 [n_seqs, width], width 1..MOE_MAX_DRAFTS).
+ * All of a sequence's rows are read before any is written, so keep may name them in any order and twice.  A place that
+ * is not there is not read, and its row is left as it was, or not written.  new_lens (nullable, not base itself): base[s] + how many
+ * were kept.  Sequences must not share the pages that are written. */
+int32_t moe_kv_compact(const moe_kv_cache* c, const int32_t* base, int32_t width, const int32_t* keep,
+                       int32_t* new_lens, void* stream);
+
+/* Pages by counts: refs (device int32 [n_pages]) says how many entries of the page table name each page; one with count 0
+ * is free.  The three calls below change the cache's page table and refs together, and keep that true.  Where pages are wanted the
+ * lowest free ones are given, in order; missing (nullable, device int32 [1]) becomes the number of those wanted that were
+ * not to be had, whose entries stay as pages that are not there (-1).  A negative length is that of a sequence that is
+ * not there.  Order on one stream; one call at a time on a table. */
+
+/* Pages of the places from lens[s] on (device int32 [n_seqs]; <= 0: all) are given back, their entries become -1. */
+int32_t moe_kv_release(const moe_kv_cache* c, int32_t* refs, const int32_t* lens, void* stream);
+
+/* Sequence dst[i] becomes another of the length and contents of sequence src[i], i < n <= n_seqs (device int32 [n]): it gives back its
+ * pages, shares src's whole ones, and has a page of its own with a copy of the places in src's last, begun one;
+ * lens[dst[i]] = lens[src[i]] (device int32 [n_seqs]).  No sequence may be dst twice, or src and dst; a pair outside
+ * 0..n_seqs-1 or of one sequence is left out.  Where the page is not to be had, the places of the begun page are not there.
+ * ws: moe_kv_pages_workspace_bytes, 256-byte aligned, need not be cleared. */
+size_t moe_kv_pages_workspace_bytes(const moe_kv_cache* c);
+int32_t moe_kv_fork(const moe_kv_cache* c, int32_t* refs, int32_t n, const int32_t* src, const int32_t* dst, int32_t* lens,
+                    int32_t* missing, void* ws, size_t ws_bytes, void* stream);
+
+/* Every entry of the places 0 .. lens[s]+more-1 of a sequence (none for lens[s] < 0, and none beyond the table) that
+ * names no page gets one: sequence after sequence, place after place. */
+int32_t moe_kv_reserve(const moe_kv_cache* c, int32_t* refs, const int32_t* lens, int32_t more, int32_t* missing,
+                       void* ws, size_t ws_bytes, void* stream);
+
+/* ---- log-probabilities of tokens ------------------------------------------- */
+
+#define MOE_MAX_ALTERNATIVES 64
+
+/* For every row of logits x [T, V] (dtype, rows row_stride elements apart, any alignment; V >= 1), with z = scale*x, scale > 0 (an inverse
+ * temperature), each nullable output (device, [T]):
+ *   lse = log sum_j exp(z_j)     logp = z_id - lse for the token ids[t]     entropy = -sum_j p_j log p_j,  p_j = exp(z_j - lse)
+ * ids device int32 [T], NULL only without logp; a token outside 0..V-1 counts for nothing: logp = 0.
+ * top_ids int32 and top_logp float [T, K] (both or none, K 0..min(V, MOE_MAX_ALTERNATIVES)): the K largest logits in falling order, equal ones by
+ * rising index, and their log-probabilities.  A NaN ranks below all else.
+ * A logit of -infinity is a token that cannot be: it adds nothing.  A row of nothing else has lse = logp = top_logp = -infinity
+ * and entropy 0; a NaN or +infinity makes lse, logp, entropy and top_logp of its row NaN.
+ * Sums are float32.  ws: moe_token_logprobs_workspace_bytes, 256-byte aligned, need not be cleared, one call at a time. */
+size_t moe_token_logprobs_workspace_bytes(int32_t T, int32_t V, int32_t K);
+int32_t moe_token_logprobs(int32_t dtype, int32_t T, int32_t V, const void* x, int64_t row_stride, float scale,
+                           const int32_t* ids, float* logp, float* lse, float* entropy, int32_t K, int32_t* top_ids,
+                           float* top_logp, void* ws, size_t ws_bytes, void* stream);
+
+/* d_x = gradient of sum_t d_logp logp + d_entropy entropy + d_lse lse (each nullable, device float [T]; d_logp needs
+ * ids, d_entropy needs entropy as the forward call gave it), with the forward call's lse:
+ *   d_x_j = scale*(d_logp ([j = id] - p_j) - d_entropy p_j (log p_j + entropy) + d_lse p_j),  rounded once to dtype.
+ * d_logp of a token outside 0..V-1 is not used.  A row whose three factors are all 0, or whose lse is -infinity, has
+ * gradient 0 whatever its logits are; a logit of -infinity has gradient 0 (d_logp*scale where it is the token's own).
+ * d_x [T, V], d_row_stride >= V elements apart; may be x itself with x's stride (row_stride >= V then), and must not overlap it otherwise. */
+int32_t moe_token_logprobs_backward(int32_t dtype, int32_t T, int32_t V, const void* x, int64_t row_stride, float scale,
+                                    const int32_t* ids, const float* lse, const float* d_logp, const float* entropy,
+                                    const float* d_entropy, const float* d_lse, void* d_x, int64_t d_row_stride,
+                                    void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -12,3 +12,7 @@ from .binding import (  # noqa: F401
 from .attention import (  # noqa: F401
     KVCache, Rotary, moe_attention_decode, moe_attention_decode_workspace_bytes, moe_kv_append, moe_rotary, rotary_freqs,
 )
+from .drafts import (  # noqa: F401
+    moe_attention_tree, moe_attention_tree_workspace_bytes, moe_kv_compact, moe_kv_fork, moe_kv_pages_workspace_bytes, moe_kv_release, moe_kv_reserve,
+)
+from .logprobs import moe_token_logprobs, moe_token_logprobs_backward, moe_token_logprobs_workspace_bytes  # noqa: F401
