@@ -28,6 +28,26 @@ MOESYS_HD uint64_t seen_drafts(bool words, uint64_t word, int i, int n) { return
 MOESYS_HD int draft_depth(uint64_t seen, int i) { return bits_set(seen & ~(1ull << i)); }
 
 // Whether a window shows place p, at position pos_p, to a token at position pos.  (Distances are below 2^31.)
-MOESYS_HD bool in_window(int pos, int pos_p, int p, int window, int sinks) { return window <= 0 || pos - pos_p < window || p < sinks; }
+MOESYS_HD bool in_window(int pos, int pos_p, int p, int window, int sinks) { return (window <= 0) | (pos - pos_p < window) | (p < sinks); }
+
+// Tiles of places that some new token can see: `sinks` of them from the first place on, then those from `from` on, `tiles` in all.
+struct Span {
+  int sinks, from, tiles;
+  MOESYS_HD int tile(int u) const { return u < sinks ? u : u - sinks + from; }
+};
+MOESYS_HD Span span_of(const Drafts& d, int window, int sinks, int tile) {
+  Span s{0, 0, 0};
+  if (d.len <= 0) return s;
+  const int upto = (d.len - 1) / tile + 1;
+  if (window > 0 && d.base >= window) {  // (no token stands before the base: what lies window or more behind it is seen by none)
+    const int from = (d.base - window + 1) / tile, shown = sinks < d.len ? sinks : d.len, front = shown > 0 ? (shown - 1) / tile + 1 : 0;
+    if (front < from) {
+      s.sinks = front;
+      s.from = from;
+    }
+  }
+  s.tiles = s.sinks + upto - s.from;
+  return s;
+}
 
 }  // namespace moesys
