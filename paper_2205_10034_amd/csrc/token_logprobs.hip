@@ -17,8 +17,8 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int THREADS = 256, WAVES = THREADS / 64;
 constexpr int PER_LANE = 16, CHUNK = 64 * PER_LANE;  // logits that a lane, a wavefront takes at a time
-constexpr int MAX_CHUNKS = 128;                      // of a part whose largest are wanted (its groups' maxima lie in LDS)
 constexpr int LIST = 128;                            // candidates that a wavefront holds
+constexpr int SHARED_LIST = 256;                     // ... that all of a row's do, and groups with candidates
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float LAG_BITS = 8.f;
 
@@ -44,19 +44,19 @@ __device__ __forceinline__ float element(const float*, const u32x4& v, int e) { 
 // -infinity, as many as 16 bytes hold
 template <typename X> constexpr uint32_t minus_infinities = sizeof(X) == 2 ? 0xff80ff80u : 0xff800000u;
 
-// per_load elements from x[j] on, -infinity in the place of those from V on
+// per_load elements from x[j] on, -infinity in the place of those that are not in 0..V-1
 template <typename X>
-__device__ __forceinline__ u32x4 load_some(const X* x, uint32_t j, int V_) {
-  const uint32_t V = (uint32_t)V_;
-  if (j + per_load<X> <= V) return reinterpret_cast<const Unaligned<X>*>(x + j)->v;
+__device__ __forceinline__ u32x4 load_some(const X* x, int64_t j, int V) {
+  if (j >= 0 && j + per_load<X> <= V) return reinterpret_cast<const Unaligned<X>*>(x + j)->v;
   u32x4 v;
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
     v[w] = minus_infinities<X>;
     if constexpr (sizeof(X) == 2) {
-      if (j + 2 * w < V) v[w] = (v[w] & 0xffff0000u) | reinterpret_cast<const uint16_t*>(x)[j + 2 * w];
-      if (j + 2 * w + 1 < V) v[w] = (v[w] & 0xffffu) | (uint32_t)reinterpret_cast<const uint16_t*>(x)[j + 2 * w + 1] << 16;
-    } else if (j + w < V) {
+      const int64_t k = j + 2 * w;
+      if (k >= 0 && k < V) v[w] = (v[w] & 0xffff0000u) | reinterpret_cast<const uint16_t*>(x)[k];
+      if (k + 1 >= 0 && k + 1 < V) v[w] = (v[w] & 0xffffu) | (uint32_t)reinterpret_cast<const uint16_t*>(x)[k + 1] << 16;
+    } else if (j + w >= 0 && j + w < V) {
       v[w] = reinterpret_cast<const uint32_t*>(x)[j + w];
     }
   }
@@ -140,43 +140,48 @@ struct RowArgs {
   float *logp, *lse, *entropy, *top_logp;
   int32_t* top_ids;
   f32x4* part_stats;   // [row][part]: m, s, e
-  uint64_t* part_keys;  // [row][part][K], falling, 0: none
-  int32_t T, V, K, parts, part_chunks;
+  char* groups;       // [row][chunk][lane]: the largest of a lane's PER_LANE logits (Group)
+  int32_t T, V, K, parts, part_chunks, max_chunks;
   float scale, c, lag;
 };
 
 // ---- the K largest -------------------------------------------------------------------------------------
 
-// Keys of one wavefront, in LDS, that are above `bound` when they come.
+// Keys of one wavefront, in LDS, that were above `bound` when they came.
 struct TopList {
   uint64_t* keys;  // [LIST]
   int n, K;
   uint64_t bound;
 
   // The K largest, in falling order; from then on only larger ones come in.
-  __device__ void sort() {
+  __device__ __forceinline__ void sort() {
     const int lane = threadIdx.x & 63;
     const uint64_t a = lane < n ? keys[lane] : 0, b = lane + 64 < n ? keys[lane + 64] : 0;
+    if (lane < 8 && n + lane < LIST) keys[n + lane] = 0;  // (above none)
+    asm volatile("" ::: "memory");                        // (a wavefront's LDS operations execute in order)
     int ra = 0, rb = 0;
-    if (n <= 64) {
-      for (int i = 0; i < n; ++i) ra += keys[i] > a;
-    } else {
-      for (int i = 0; i < n; ++i) {
-        const uint64_t k = keys[i];
-        ra += k > a;
-        rb += k > b;
-      }
+    for (int i = 0; i < n; i += 8) {
+      uint64_t k[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) k[e] = keys[i + e];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ra += k[e] > a;
+      if (n > 64)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) rb += k[e] > b;
     }
-    asm volatile("" ::: "memory");  // (a wavefront's LDS operations execute in order)
+    asm volatile("" ::: "memory");
     if (lane < n && ra < K) keys[ra] = a;
     if (lane + 64 < n && rb < K) keys[rb] = b;
     asm volatile("" ::: "memory");
     if (n >= K) {
       n = K;
       bound = keys[K - 1];
+      bound = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(bound >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)bound);
     }
   }
 
+  // A key of each lane that has one.
   __device__ __forceinline__ void offer(bool have, uint64_t key) {
     unsigned long long all = __ballot(have && key > bound);
     if (!all) return;
@@ -190,161 +195,204 @@ struct TopList {
   }
 };
 
-// The K-th and the K2-th largest of the lanes' values (0: no value), a little less, or 0 where there are fewer.
-__device__ __forceinline__ void largest_lanes(uint32_t u, int K, int K2, uint32_t& first, uint32_t& second) {
-  const int lane = threadIdx.x & 63;
-  const uint32_t mine = (u & ~63u) | (63 - lane);  // all differ
-  int rank = 0;
-#pragma unroll 16
-  for (int i = 0; i < 64; ++i) rank += (uint32_t)__builtin_amdgcn_readlane((int)mine, i) > mine;
-  auto of_rank = [&](int r) {
-    const unsigned long long who = __ballot(rank == r);
-    return (uint32_t)__builtin_amdgcn_readlane((int)mine, (int)__ffsll(who) - 1) & ~63u;
-  };
-  first = of_rank(K - 1);
-  second = of_rank(K2 - 1);
+// A value that K of the lanes' (0: no value) reach: their K-th largest, cut down to the upper BITS bits.
+template <int BITS>
+__device__ __forceinline__ uint32_t reached_by(uint32_t u, int K) {
+  uint32_t t = 0;
+#pragma unroll
+  for (int bit = 31; bit >= 32 - BITS; --bit) {
+    const uint32_t more = t | 1u << bit;
+    t = __popcll(__ballot(u >= more)) >= K ? more : t;
+  }
+  return t;
 }
 
-// The largest logit of a lane's PER_LANE, as LDS keeps it: a bfloat16's order is told by its upper half.
+// The largest logit of a lane's PER_LANE, as it is kept: a bfloat16's order is told by its upper half.
 template <typename X> struct Group;
 template <> struct Group<__bf16> {
   typedef uint16_t type;
+  static constexpr int BITS = 16;  // of an order that tell groups apart
   static __device__ __forceinline__ uint16_t pack(uint32_t order) { return (uint16_t)(order >> 16); }
   static __device__ __forceinline__ uint32_t order(uint16_t g) { return (uint32_t)g << 16 | (g & 0x8000u ? 0u : 0xffffu); }
+  static __device__ __forceinline__ uint32_t order(const u32x4& v, int e) { return order((uint16_t)(v[e / 2] >> (e & 1 ? 16 : 0))); }
 };
 template <> struct Group<float> {
   typedef uint32_t type;
+  static constexpr int BITS = 24;
   static __device__ __forceinline__ uint32_t pack(uint32_t order) { return order; }
   static __device__ __forceinline__ uint32_t order(uint32_t g) { return g; }
+  static __device__ __forceinline__ uint32_t order(const u32x4& v, int e) { return v[e]; }
 };
 
-// The K largest of a part (chunks c0 .. c0+n-1 of the row) into the list, by one wavefront: of the groups whose largest logit can be among them,
-// 64 at a time, a group to a lane.
+// First element of load l of lane `lane` in chunk c of a row whose first logit is `back` elements behind a multiple of 16 bytes.
 template <typename X>
-__device__ void find_largest(TopList& top, const typename Group<X>::type* group_max, uint32_t* found, const X* x, int V, int c0, int n) {
+__device__ __forceinline__ int64_t index_of(int c, int l, int lane, int back) { return (int64_t)c * CHUNK + (l * 64 + lane) * per_load<X> - back; }
+
+// A row whose largest logits are wanted.
+template <typename X> struct Candidates {
+  const X* x;
+  const typename Group<X>::type* groups;
+  int V, back, chunks;
+
+  // No logit of a group has a larger key than its largest would have in the group's first place.
+  __device__ __forceinline__ uint64_t best_key(uint32_t order, int group) const {
+    const int64_t j = index_of<X>(group >> 6, 0, group & 63, back);
+    return key_of(order, j > 0 ? (int)j : 0);
+  }
+};
+
+// Lanes' places behind one another, `mine` (up to PER_LANE) to each, and how many there are: a ballot per bit.
+__device__ __forceinline__ void places(int mine, int& before, int& all) {
+  before = all = 0;
+#pragma unroll
+  for (int bit = 0; 1 << bit <= PER_LANE; ++bit) {
+    const unsigned long long with = __ballot(mine >> bit & 1);
+    before += __popcll(with & ((1ull << (threadIdx.x & 63)) - 1)) << bit;
+    all += __popcll(with) << bit;
+  }
+}
+
+// The logits of `count` (up to 64) groups into the list, a group to a lane.
+template <typename X>
+__device__ __forceinline__ void offer_groups(TopList& top, const uint32_t* found, int count, const Candidates<X>& p) {
+  constexpr int N = per_load<X>;
+  const int lane = threadIdx.x & 63;
+  const bool have = lane < count;
+  const uint32_t at = have ? found[lane] : 0;
+  const int64_t j0 = index_of<X>(at >> 6, 0, at & 63, p.back);
+#pragma unroll 1
+  for (int l = 0; l < loads<X>; ++l) {
+    const int64_t j = j0 + l * 64 * N;
+    const u32x4 v = have ? load_some(p.x, j, p.V) : u32x4{0, 0, 0, 0};
+    uint32_t order[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) order[e] = order_of(element((const X*)nullptr, v, e));
+    // All of them at once, or, where the list cannot hold them even after it was sorted (many equal or rising ones), one of each lane.
+    uint32_t left = (1u << N) - 1, now = left;
+    while (left) {
+      uint32_t mask = 0;
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (j + e >= 0 && j + e < p.V && key_of(order[e], (int)(j + e)) > top.bound) mask |= 1u << e;
+      mask = have ? mask & now : 0;
+      int before, all;
+      places(__popc(mask), before, all);
+      before += top.n;
+      if (top.n + all > LIST) {
+        if (top.n > top.K) top.sort();
+        else now = left & (0u - left);
+        continue;
+      }
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (mask >> e & 1) top.keys[before++] = key_of(order[e], (int)(j + e));
+      top.n += all;
+      asm volatile("" ::: "memory");
+      left &= ~now;
+      now = left;
+    }
+  }
+}
+
+// The K largest of a row by one wavefront, chunk after chunk, where candidates are many (equal or rising logits): the bound rises on the way.
+template <typename X>
+__device__ __forceinline__ void find_in_order(TopList& top, uint32_t* found, const Candidates<X>& p) {
   const int lane = threadIdx.x & 63;
   int count = 0;
-  auto flush = [&]() {
+  for (int c = 0;;) {
+    for (; c < p.chunks; ++c) {
+      const bool can = p.best_key(Group<X>::order(p.groups[(int64_t)c * 64 + lane]), c * 64 + lane) > top.bound;
+      const unsigned long long all = __ballot(can);
+      if (count + __popcll(all) > 64) break;
+      if (can) found[count + __popcll(all & ((1ull << lane) - 1))] = c * 64 + lane;
+      count += __popcll(all);
+    }
     asm volatile("" ::: "memory");
-    const bool have = lane < count;
-    const uint32_t at = have ? found[lane] : 0, j0 = (at >> 6) * CHUNK + (at & 63) * per_load<X>;
-    u32x4 v[loads<X>];
-#pragma unroll
-    for (int l = 0; l < loads<X>; ++l) v[l] = have ? load_some(x, j0 + l * 64 * per_load<X>, V) : u32x4{0, 0, 0, 0};
-#pragma unroll
-    for (int l = 0; l < loads<X>; ++l)
-#pragma unroll
-      for (int e = 0; e < per_load<X>; ++e) {
-        const uint32_t j = j0 + l * 64 * per_load<X> + e;
-        top.offer(have && j < (uint32_t)V, key_of(order_of(element((const X*)nullptr, v[l], e)), j));
-      }
+    offer_groups<X>(top, found, count, p);
+    if (c >= p.chunks) break;
     count = 0;
-  };
-  for (int c = 0; c < n; ++c) {
-    // (no logit of the group has a larger key than its largest would have in the group's first place)
-    const uint32_t at = (uint32_t)(c0 + c) * 64 + lane;
-    const bool can = key_of(Group<X>::order(group_max[c * 64 + lane]), (at >> 6) * CHUNK + lane * per_load<X>) > top.bound;
-    const unsigned long long all = __ballot(can);
-    if (!all) continue;
-    if (count + __popcll(all) > 64) flush();
-    if (can) found[count + __popcll(all & ((1ull << lane) - 1))] = at;
-    count += __popcll(all);
   }
-  if (count) flush();
   top.sort();
 }
 
 // ---- forward -------------------------------------------------------------------------------------------
 
-template <typename X, bool ENTROPY, bool TOP>
-__device__ __forceinline__ void finish_row(const RowArgs& a, int t, const Stats& st, X id_logit, int id, const TopList& top) {
-  const int lane = threadIdx.x & 63;
-  const Row row(st, a.scale);
-  if (lane == 0) {
-    if (a.lse) a.lse[t] = row.lse();
-    if (a.logp) a.logp[t] = (unsigned)id < (unsigned)a.V ? row.logp((float)id_logit) : 0.f;
-    if (ENTROPY) a.entropy[t] = row.entropy(st);
-  }
-  if (TOP && lane < a.K) {
-    const uint64_t key = top.keys[lane];
-    a.top_ids[(int64_t)t * a.K + lane] = (int)~(uint32_t)key;
-    a.top_logp[(int64_t)t * a.K + lane] = row.logp(of_order((uint32_t)(key >> 32)));
-  }
+template <bool ENTROPY>
+__device__ __forceinline__ void store_row(const RowArgs& a, int t, const Stats& st, const Row& row, float id_logit, int id) {
+  if (a.lse) a.lse[t] = row.lse();
+  if (a.logp) a.logp[t] = (unsigned)id < (unsigned)a.V ? row.logp(id_logit) : 0.f;
+  if (ENTROPY) a.entropy[t] = row.entropy(st);
 }
 
-// TEAM wavefronts to a part of a row, chunk after chunk in turn; their first one ends it.
+// TEAM wavefronts to a part of a row, chunk after chunk in turn; their first one ends it.  TOP: groups' maxima are kept for select_kernel,
+// which ends the rows.
 template <typename X, int TEAM, bool ENTROPY, bool TOP>
 __global__ __launch_bounds__(THREADS) void rows_kernel(RowArgs a) {
   using G = Group<X>;
-  extern __shared__ __attribute__((aligned(16))) char group_lds[];
-  __shared__ uint64_t keys[TOP ? WAVES / TEAM : 1][TOP ? LIST : 1];
-  __shared__ uint32_t found[TOP ? WAVES / TEAM : 1][64];
   __shared__ Stats stats[WAVES];
-  __shared__ uint32_t bounds[WAVES][2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), team = wave / TEAM, me = wave % TEAM;
   const unsigned unit = blockIdx.x * (WAVES / TEAM) + team;
   const int t = TEAM == 1 ? (int)unit : (int)(unit / (unsigned)a.parts), part = TEAM == 1 ? 0 : (int)(unit - (unsigned)t * (unsigned)a.parts);
   if (TEAM == 1 && t >= a.T) return;
+  const bool ends = !TOP && a.parts == 1;
   const X* x = reinterpret_cast<const X*>(a.x + (int64_t)t * a.row_stride);
-  const int c0 = part * a.part_chunks, all_chunks = (a.V - 1) / CHUNK + 1, c1 = c0 + a.part_chunks < all_chunks ? c0 + a.part_chunks : all_chunks;
-  const int whole = a.V / CHUNK < c1 ? a.V / CHUNK : c1;  // chunks that end inside the row
-  typename G::type* group_max = reinterpret_cast<typename G::type*>(group_lds) + team * a.part_chunks * 64;
+  // chunks lie on multiples of 16 bytes (rows of 50001 bfloat16 logits are read at 4.4 TB/s from their own beginnings on, at 5.7 so)
+  const int back = (int)((uintptr_t)x & 15) / (int)sizeof(X), all_chunks = (int)(((int64_t)a.V + back - 1) / CHUNK) + 1;
+  const int c0 = part * a.part_chunks, c1 = c0 + a.part_chunks < all_chunks ? c0 + a.part_chunks : all_chunks;
+  const int inside = (int)(((int64_t)a.V + back) / CHUNK), whole = inside < c1 ? inside : c1;  // chunks that end in the row
+  typename G::type* groups = reinterpret_cast<typename G::type*>(a.groups) + (int64_t)t * a.max_chunks * 64;
 
   // the token's own logit, ahead of need
   int id = -1;
   X id_logit{};
-  if (a.logp && a.parts == 1 && me == 0) {
+  if (ends && a.logp && me == 0) {
     id = a.ids[t];
     id_logit = x[(unsigned)id < (unsigned)a.V ? id : 0];
   }
 
   Stats st{-INFINITY, 0.f, 0.f};
-  float lane_top = -INFINITY;
   auto take = [&](int c, const u32x4 (&v)[loads<X>]) {
     const float top = take_chunk<X, ENTROPY>(st, v, a.c, a.lag);
-    if (TOP) {
-      group_max[(c - c0) * 64 + lane] = G::pack(order_of(top));
-      lane_top = fmaxf(lane_top, top);
-    }
+    if (TOP) groups[(int64_t)c * 64 + lane] = G::pack(order_of(top));
   };
-  int c = c0 + me;
-  if (c < whole) {
-    u32x4 next[loads<X>];
-    load_chunk(x + (int64_t)c * CHUNK, next);
-    for (; c + TEAM < whole; c += TEAM) {
-      u32x4 v[loads<X>];
-#pragma unroll
-      for (int l = 0; l < loads<X>; ++l) v[l] = next[l];
-      load_chunk(x + (int64_t)(c + TEAM) * CHUNK, next);
-      take(c, v);
-    }
-    take(c, next);
-    c += TEAM;
-  }
-  if (c < c1) {
+  // (two chunks' loads stay in flight; one that would begin behind the last whole chunk is that one's again)
+  auto take_some = [&](int c) {
     u32x4 v[loads<X>];
 #pragma unroll
-    for (int l = 0; l < loads<X>; ++l) v[l] = load_some(x, c * CHUNK + first_of<X>(l), a.V);
+    for (int l = 0; l < loads<X>; ++l) v[l] = load_some(x, index_of<X>(c, l, lane, back), a.V);
     take(c, v);
+  };
+  int c = c0 + me;
+  if (c == 0 && back && whole > 0) {
+    take_some(0);
+    c += TEAM;
   }
-  join_lanes<ENTROPY>(st, a.c);
-  uint32_t first = 0, second = 0;
-  if (TOP) largest_lanes(lane_top == -INFINITY ? 0u : order_of(lane_top), a.K, (a.K - 1) / TEAM + 1, first, second);
-  if (TEAM > 1) {
-    if (lane == 0) {
-      stats[wave] = st;
-      bounds[wave][0] = first;
-      bounds[wave][1] = second;
+  if (c < whole) {
+    u32x4 even[loads<X>], odd[loads<X>];
+    const int last = c + (whole - 1 - c) / TEAM * TEAM;
+    auto load = [&](int at, u32x4 (&v)[loads<X>]) { load_chunk(x + ((int64_t)(at < last ? at : last) * CHUNK - back), v); };
+    load(c, even);
+    load(c + TEAM, odd);
+    for (; c + TEAM <= last; c += 2 * TEAM) {
+      take(c, even);
+      load(c + 2 * TEAM, even);
+      take(c + TEAM, odd);
+      load(c + 3 * TEAM, odd);
     }
+    if (c == last) {
+      take(c, even);
+      c += TEAM;
+    }
+  }
+  if (c < c1) take_some(c);
+  join_lanes<ENTROPY>(st, a.c);
+  if (TEAM > 1) {
+    if (lane == 0) stats[wave] = st;
     lds_barrier();
     if (me != 0) return;
     float m = stats[0].m;
 #pragma unroll
-    for (int w = 1; w < TEAM; ++w) {
-      m = fmaxf(m, stats[w].m);
-      first = bounds[w][0] > first ? bounds[w][0] : first;
-      second = bounds[w][1] < second ? bounds[w][1] : second;
-    }
+    for (int w = 1; w < TEAM; ++w) m = fmaxf(m, stats[w].m);
     refer<ENTROPY>(st, m, a.c);
 #pragma unroll
     for (int w = 1; w < TEAM; ++w) {
@@ -354,79 +402,189 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(RowArgs a) {
       st.e += other.e;
     }
   }
-  // At least K logits of the part reach the larger of these: K lanes of one wavefront do, or a K-th of them in each.
-  TopList top{keys[TOP ? team : 0], 0, a.K, (uint64_t)(first > second ? first : second) << 32};
-  if (TOP) find_largest<X>(top, group_max, found[team], x, a.V, c0, c1 - c0);
-  if (a.parts == 1) {
-    finish_row<X, ENTROPY, TOP>(a, t, st, id_logit, id, top);
-  } else {
-    if (lane == 0) a.part_stats[unit] = f32x4{st.m, st.s, st.e, 0.f};
-    if (TOP && lane < a.K) a.part_keys[(int64_t)unit * a.K + lane] = lane < top.n ? top.keys[lane] : 0;
-  }
+  if (lane != 0) return;
+  if (ends) store_row<ENTROPY>(a, t, st, Row(st, a.scale), (float)id_logit, id);
+  else a.part_stats[unit] = f32x4{st.m, st.s, st.e, 0.f};
 }
 
-// A wavefront to a row: its parts' sums, in order of the lanes that read them, and the largest of their largest.
-template <typename X, bool ENTROPY, bool TOP>
-__global__ __launch_bounds__(64) void join_kernel(RowArgs a) {
-  __shared__ uint64_t keys[TOP ? LIST : 1];
-  const int t = blockIdx.x, lane = threadIdx.x;
-  const X* x = reinterpret_cast<const X*>(a.x + (int64_t)t * a.row_stride);
-  int id = -1;
-  X id_logit{};
-  if (a.logp) {
-    id = a.ids[t];
-    id_logit = x[(unsigned)id < (unsigned)a.V ? id : 0];
-  }
-  const int64_t unit = (int64_t)t * a.parts;
-  const uint64_t* part_keys = a.part_keys + unit * a.K;
-  Stats st{-INFINITY, 0.f, 0.f};
-  uint64_t first = 0, second = ~0ull;
-  for (int p = lane; p < a.parts; p += 64) {
-    const f32x4 v = a.part_stats[unit + p];
+// A row's sums from its parts', in order of the lanes that read them; `mine`: those of the lane's first part, read ahead.
+__device__ __forceinline__ f32x4 first_part(const RowArgs& a, int t) {
+  const int lane = threadIdx.x & 63;
+  return lane < a.parts ? a.part_stats[(int64_t)t * a.parts + lane] : f32x4{-INFINITY, 0.f, 0.f, 0.f};
+}
+template <bool ENTROPY>
+__device__ __forceinline__ Stats join_parts(const RowArgs& a, int t, const f32x4& mine) {
+  Stats st{mine[0], mine[1], mine[2]};
+  for (int p = 64 + (threadIdx.x & 63); p < a.parts; p += 64) {
+    const f32x4 v = a.part_stats[(int64_t)t * a.parts + p];
     Stats other{v[0], v[1], v[2]};
     const float m = fmaxf(st.m, other.m);
     refer<ENTROPY>(st, m, a.c);
     refer<ENTROPY>(other, m, a.c);
     st.s += other.s;
     st.e += other.e;
-    if (TOP) {
-      const uint64_t last = part_keys[(int64_t)p * a.K + a.K - 1], some = part_keys[(int64_t)p * a.K + (a.K - 1) / a.parts];
-      first = last > first ? last : first;
-      second = some < second ? some : second;
-    }
   }
   join_lanes<ENTROPY>(st, a.c);
-  TopList top{keys, 0, a.K, 0};
-  if (TOP) {
-    for (int d = 32; d; d >>= 1) {
-      const uint64_t f = __shfl_xor(first, d, 64), s = __shfl_xor(second, d, 64);
-      first = f > first ? f : first;
-      second = s < second ? s : second;
-    }
-    const uint64_t reached = first > second ? first : second;
-    top.bound = reached ? reached - 1 : 0;
-    const int64_t n = (int64_t)a.parts * a.K;
-    constexpr int AHEAD = 4;
-    for (int64_t i = lane; i - lane < n; i += 64 * AHEAD) {
-      uint64_t k[AHEAD];
-#pragma unroll
-      for (int e = 0; e < AHEAD; ++e) k[e] = i + e * 64 < n ? part_keys[i + e * 64] : 0;
-#pragma unroll
-      for (int e = 0; e < AHEAD; ++e) top.offer(k[e] != 0, k[e]);
-    }
-    top.sort();
+  return st;
+}
+
+// Ends the rows that lay in several parts, a wavefront to a row.
+template <typename X, bool ENTROPY>
+__global__ __launch_bounds__(64) void join_kernel(RowArgs a) {
+  const int t = blockIdx.x;
+  int id = -1;
+  X id_logit{};
+  if (a.logp) {
+    id = a.ids[t];
+    id_logit = reinterpret_cast<const X*>(a.x + (int64_t)t * a.row_stride)[(unsigned)id < (unsigned)a.V ? id : 0];
   }
-  finish_row<X, ENTROPY, TOP>(a, t, st, id_logit, id, top);
+  const Stats st = join_parts<ENTROPY>(a, t, first_part(a, t));
+  if (threadIdx.x == 0) store_row<ENTROPY>(a, t, st, Row(st, a.scale), (float)id_logit, id);
+}
+
+// Ends the rows whose K largest logits are wanted, a workgroup of TEAM wavefronts to a row.  A bound that K of the threads' largest groups
+// reach leaves little more than K groups; their logits above it, in LDS, are ranked by counting, a key to a thread.
+template <typename X, int TEAM, bool ENTROPY>
+__global__ __launch_bounds__(64 * TEAM) void select_kernel(RowArgs a) {
+  using G = Group<X>;
+  constexpr int N = 64 * TEAM, PER = 16 / (int)sizeof(typename G::type);
+  __shared__ __attribute__((aligned(16))) uint64_t keys[SHARED_LIST];
+  __shared__ uint32_t found[SHARED_LIST];
+  __shared__ uint32_t bounds[TEAM][2];
+  __shared__ int n_found, n_keys;
+  const int t = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const X* x = reinterpret_cast<const X*>(a.x + (int64_t)t * a.row_stride);
+  const int back = (int)((uintptr_t)x & 15) / (int)sizeof(X);
+  const Candidates<X> row{x, reinterpret_cast<const typename G::type*>(a.groups) + (int64_t)t * a.max_chunks * 64, a.V, back, (int)(((int64_t)a.V + back - 1) / CHUNK) + 1};
+  int id = -1;
+  X id_logit{};
+  if (a.logp) {
+    id = a.ids[t];
+    id_logit = x[(unsigned)id < (unsigned)a.V ? id : 0];
+  }
+  if (threadIdx.x == 0) n_found = n_keys = 0;
+  const f32x4 mine = first_part(a, t);
+  // Groups: 16 bytes of them to a thread (chunks have 64), or, of short rows, single ones, so that most threads have some.
+  const int n_groups = row.chunks * 64;
+  const bool single = row.chunks <= 8 * TEAM;
+  uint32_t best = 0;
+  if (single) {
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n_groups; i += N) {
+      const uint32_t order = G::order(row.groups[i]);
+      best = order > best ? order : best;
+    }
+  } else {
+#pragma unroll 2
+    for (int i = threadIdx.x * PER; i < n_groups; i += N * PER) {
+      const u32x4 v = *reinterpret_cast<const u32x4*>(row.groups + i);
+#pragma unroll
+      for (int e = 0; e < PER; ++e) best = G::order(v, e) > best ? G::order(v, e) : best;
+    }
+  }
+  // (-infinity and NaN bound nothing)
+  if (best <= order_of(-INFINITY)) best = 0;
+  uint32_t first = reached_by<G::BITS>(best, a.K), second = first;
+  if (TEAM > 1) {
+    second = reached_by<G::BITS>(best, (a.K - 1) / TEAM + 1);
+    if (lane == 0) {
+      bounds[wave][0] = first;
+      bounds[wave][1] = second;
+    }
+    lds_barrier();
+#pragma unroll
+    for (int w = 0; w < TEAM; ++w) {
+      first = bounds[w][0] > first ? bounds[w][0] : first;
+      second = bounds[w][1] < second ? bounds[w][1] : second;
+    }
+  }
+  // At least K logits reach the larger of these: K threads of one wavefront do, or a TEAM-th of K in each.
+  const uint32_t bound = first > second ? first : second;
+  if (single) {
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n_groups; i += N)
+      if (G::order(row.groups[i]) >= bound) {
+        const int at = atomicAdd(&n_found, 1);
+        if (at < SHARED_LIST) found[at] = i;
+      }
+  } else {
+#pragma unroll 2
+    for (int i = threadIdx.x * PER; i < n_groups; i += N * PER) {
+      const u32x4 v = *reinterpret_cast<const u32x4*>(row.groups + i);
+#pragma unroll
+      for (int e = 0; e < PER; ++e)
+        if (G::order(v, e) >= bound) {
+          const int at = atomicAdd(&n_found, 1);
+          if (at < SHARED_LIST) found[at] = i + e;
+        }
+    }
+  }
+  const Stats st = join_parts<ENTROPY>(a, t, mine);
+  const Row sums(st, a.scale);
+  if (threadIdx.x == 0) store_row<ENTROPY>(a, t, st, sums, (float)id_logit, id);
+  auto store = [&](int rank, uint64_t key) {
+    a.top_ids[(int64_t)t * a.K + rank] = (int)~(uint32_t)key;
+    a.top_logp[(int64_t)t * a.K + rank] = sums.logp(of_order((uint32_t)(key >> 32)));
+  };
+  lds_barrier();
+  const int groups = n_found;
+  if (groups <= SHARED_LIST) {
+    for (int i0 = wave * 64; i0 < groups; i0 += N) {
+      const bool have = i0 + lane < groups;
+      const uint32_t at = have ? found[i0 + lane] : 0;
+      const int64_t j0 = index_of<X>(at >> 6, 0, at & 63, back);
+      u32x4 v[loads<X>];
+      uint32_t mask = 0;
+#pragma unroll
+      for (int l = 0; l < loads<X>; ++l) v[l] = load_some(x, j0 + l * 64 * per_load<X>, a.V);
+#pragma unroll
+      for (int l = 0; l < loads<X>; ++l)
+#pragma unroll
+        for (int e = 0; e < per_load<X>; ++e) {
+          const int64_t j = j0 + l * 64 * per_load<X> + e;
+          mask |= (uint32_t)((j >= 0) & (j < a.V) & (order_of(element((const X*)nullptr, v[l], e)) >= bound)) << (l * per_load<X> + e);
+        }
+      int place, all;
+      places(have ? __popc(mask) : 0, place, all);
+      int begin = lane == 0 ? atomicAdd(&n_keys, all) : 0;
+      place += __builtin_amdgcn_readfirstlane(begin);
+      if (!have || place + __popc(mask) > SHARED_LIST) mask = 0;
+#pragma unroll
+      for (int l = 0; l < loads<X>; ++l)
+#pragma unroll
+        for (int e = 0; e < per_load<X>; ++e)
+          if (mask >> (l * per_load<X> + e) & 1) keys[place++] = key_of(order_of(element((const X*)nullptr, v[l], e)), (int)(j0 + l * 64 * per_load<X> + e));
+    }
+    lds_barrier();
+    const int n = n_keys;
+    if (n <= SHARED_LIST) {
+      for (int i = n + threadIdx.x; i < ((n + 7) & ~7); i += N) keys[i] = 0;  // (above none)
+      lds_barrier();
+      for (int i0 = wave * 64; i0 < n; i0 += N) {
+        const uint64_t my_key = i0 + lane < n ? keys[i0 + lane] : ~0ull;
+        int rank = 0;
+        for (int i = 0; i < n; i += 8)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) rank += keys[i + e] > my_key;
+        if (i0 + lane < n && rank < a.K) store(rank, my_key);
+      }
+      return;
+    }
+  }
+  if (wave != 0) return;
+  TopList top{keys, 0, a.K, (uint64_t)bound << 32};
+  find_in_order<X>(top, found, row);
+  if (lane < a.K) store(lane, keys[lane]);
 }
 
 // How a call's rows are divided.
 struct Division {
-  int team, parts, part_chunks;
-  size_t keys, total;  // bytes
+  int team, parts, part_chunks, max_chunks;
+  size_t groups, total;  // bytes
 };
 Division division_of(int T, int V, int K) {
-  const int chunks = (V - 1) / CHUNK + 1;
-  Division d{chunks <= 2 ? 1 : WAVES, 1, chunks, 0, 256};
+  const int chunks = (int)(((int64_t)V + 6) / CHUNK) + 1;  // of a row that begins just before a multiple of 16 bytes
+  Division d{chunks <= 2 ? 1 : WAVES, 1, chunks, chunks, 0, 256};
   if (chunks > 16) {
     int64_t parts = T > 0 ? 2048 / T : 1;
     const int64_t most = (chunks + 7) / 8;
@@ -434,26 +592,30 @@ Division division_of(int T, int V, int K) {
     if (parts < 1) parts = 1;
     d.part_chunks = (int)((chunks + parts - 1) / parts);
     d.part_chunks = (d.part_chunks + WAVES - 1) / WAVES * WAVES;
-    if (K > 0 && d.part_chunks > MAX_CHUNKS) d.part_chunks = MAX_CHUNKS;
     d.parts = (chunks - 1) / d.part_chunks + 1;
   }
-  if (d.parts > 1) {
-    d.keys = align_up((size_t)T * d.parts * sizeof(f32x4), 256);
-    d.total = d.keys + align_up((size_t)T * d.parts * K * sizeof(uint64_t), 256);
-    if (d.total < 256) d.total = 256;
-  }
+  if (d.parts > 1 || K > 0) d.total = d.groups = align_up((size_t)T * d.parts * sizeof(f32x4), 256);
+  if (K > 0) d.total += (size_t)T * chunks * 64 * sizeof(uint32_t);
+  if (d.total < 256) d.total = 256;
   return d;
 }
+
+// Whether one wavefront finds a row's largest: of short rows, with several lanes to each of the K, or the bound is too low.
+bool select_alone(int chunks, int K) { return chunks <= 2 || (chunks <= 8 && K <= 16); }
 
 template <typename X, bool ENTROPY, bool TOP>
 int32_t launch_rows(const RowArgs& a, const Division& d, hipStream_t s) {
   const int64_t units = (int64_t)a.T * d.parts;
-  const size_t lds = TOP ? (size_t)(WAVES / d.team) * d.part_chunks * 64 * sizeof(typename Group<X>::type) : 0;
-  if (d.team == 1) hipLaunchKernelGGL((rows_kernel<X, 1, ENTROPY, TOP>), dim3((unsigned)((units + WAVES - 1) / WAVES)), dim3(THREADS), lds, s, a);
-  else hipLaunchKernelGGL((rows_kernel<X, WAVES, ENTROPY, TOP>), dim3((unsigned)units), dim3(THREADS), lds, s, a);
+  if (d.team == 1) hipLaunchKernelGGL((rows_kernel<X, 1, ENTROPY, TOP>), dim3((unsigned)((units + WAVES - 1) / WAVES)), dim3(THREADS), 0, s, a);
+  else hipLaunchKernelGGL((rows_kernel<X, WAVES, ENTROPY, TOP>), dim3((unsigned)units), dim3(THREADS), 0, s, a);
   int32_t st = check_hip(hipGetLastError(), "log-probabilities launch");
-  if (st != MOE_OK || d.parts == 1) return st;
-  hipLaunchKernelGGL((join_kernel<X, ENTROPY, TOP>), dim3((unsigned)a.T), dim3(64), 0, s, a);
+  if (st != MOE_OK || (d.parts == 1 && !TOP)) return st;
+  if constexpr (TOP) {
+    if (select_alone(d.max_chunks, a.K)) hipLaunchKernelGGL((select_kernel<X, 1, ENTROPY>), dim3((unsigned)a.T), dim3(64), 0, s, a);
+    else hipLaunchKernelGGL((select_kernel<X, WAVES, ENTROPY>), dim3((unsigned)a.T), dim3(64 * WAVES), 0, s, a);
+  } else {
+    hipLaunchKernelGGL((join_kernel<X, ENTROPY>), dim3((unsigned)a.T), dim3(64), 0, s, a);
+  }
   return check_hip(hipGetLastError(), "log-probabilities join launch");
 }
 
@@ -516,7 +678,7 @@ __global__ __launch_bounds__(THREADS) void gradient_kernel(GradArgs a) {
   if (lse == -INFINITY || (g == 0.f && ge == 0.f && gl == 0.f)) {
     for (int c = c0; c < c1; ++c)
 #pragma unroll
-      for (int l = 0; l < loads<X>; ++l) store_some(y, c * CHUNK + first_of<X>(l), a.V, u32x4{0, 0, 0, 0});
+      for (int l = 0; l < loads<X>; ++l) store_some(y, (uint32_t)c * CHUNK + first_of<X>(l), a.V, u32x4{0, 0, 0, 0});
     return;
   }
   const float h = ge != 0.f ? a.entropy[t] : 0.f;
@@ -541,7 +703,7 @@ __global__ __launch_bounds__(THREADS) void gradient_kernel(GradArgs a) {
   for (int c = c0; c < c1; ++c) {
     u32x4 v[loads<X>];
 #pragma unroll
-    for (int l = 0; l < loads<X>; ++l) v[l] = load_some(x, c * CHUNK + first_of<X>(l), a.V);
+    for (int l = 0; l < loads<X>; ++l) v[l] = load_some(x, (int64_t)c * CHUNK + first_of<X>(l), a.V);
     take(c, v);
   }
 }
@@ -584,7 +746,7 @@ extern "C" int32_t moe_token_logprobs(int32_t dtype, int32_t T, int32_t V, const
   const Division d = division_of(T, V, K);
   if (!launchable((int64_t)T * d.parts, THREADS)) return fail(MOE_ERR_UNSUPPORTED, "moe_token_logprobs: %d rows are too many for one call", T);
   const float c = fminf(scale * LOG2E, FLT_MAX);
-  const RowArgs a{(const char*)x, row_stride * (int64_t)es, ids, logp, lse, entropy, top_logp, top_ids, (f32x4*)ws, (uint64_t*)((char*)ws + d.keys), T, V, K, d.parts, d.part_chunks, scale, c, LAG_BITS / c};
+  const RowArgs a{(const char*)x, row_stride * (int64_t)es, ids, logp, lse, entropy, top_logp, top_ids, (f32x4*)ws, (char*)ws + d.groups, T, V, K, d.parts, d.part_chunks, d.max_chunks, scale, c, LAG_BITS / c};
   return dtype == MOE_BF16 ? launch_rows<__bf16>(a, d, (hipStream_t)stream) : launch_rows<float>(a, d, (hipStream_t)stream);
 }
 
