@@ -21,6 +21,7 @@ constexpr int LIST = 128;                            // candidates that a wavefr
 constexpr int SHARED_LIST = 256;                     // ... that all of a row's do, and groups with candidates
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float LAG_BITS = 8.f;
+constexpr float FAR = 1024.f;  // 2^-14 of p is what lse's rounding is there
 
 // 16 bytes of logits at any alignment of their elements
 template <typename X> struct __attribute__((packed, aligned(sizeof(X)))) Unaligned {
@@ -224,7 +225,12 @@ template <> struct Group<float> {
   static __device__ __forceinline__ uint32_t order(const u32x4& v, int e) { return v[e]; }
 };
 
-// First element of load l of lane `lane` in chunk c of a row whose first logit is `back` elements behind a multiple of 16 bytes.
+// Elements by which a row begins behind a multiple of `line` bytes, on which its chunks lie; and chunks of a row of V elements, at most.
+template <typename X>
+__device__ __forceinline__ int elements_behind(const X* x, int line) { return (int)((uintptr_t)x & (line - 1)) / (int)sizeof(X); }
+int most_chunks(int V, int line, int elem) { return (int)(((int64_t)V + line / elem - 2) / CHUNK) + 1; }
+
+// First element of load l of lane `lane` in chunk c of a row that begins `back` elements behind a chunk's beginning.
 template <typename X>
 __device__ __forceinline__ int64_t index_of(int c, int l, int lane, int back) { return (int64_t)c * CHUNK + (l * 64 + lane) * per_load<X> - back; }
 
@@ -337,7 +343,7 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(RowArgs a) {
   const bool ends = !TOP && a.parts == 1;
   const X* x = reinterpret_cast<const X*>(a.x + (int64_t)t * a.row_stride);
   // chunks lie on multiples of 16 bytes (rows of 50001 bfloat16 logits are read at 4.4 TB/s from their own beginnings on, at 5.7 so)
-  const int back = (int)((uintptr_t)x & 15) / (int)sizeof(X), all_chunks = (int)(((int64_t)a.V + back - 1) / CHUNK) + 1;
+  const int back = elements_behind(x, 16), all_chunks = (int)(((int64_t)a.V + back - 1) / CHUNK) + 1;
   const int c0 = part * a.part_chunks, c1 = c0 + a.part_chunks < all_chunks ? c0 + a.part_chunks : all_chunks;
   const int inside = (int)(((int64_t)a.V + back) / CHUNK), whole = inside < c1 ? inside : c1;  // chunks that end in the row
   typename G::type* groups = reinterpret_cast<typename G::type*>(a.groups) + (int64_t)t * a.max_chunks * 64;
@@ -454,7 +460,7 @@ __global__ __launch_bounds__(64 * TEAM) void select_kernel(RowArgs a) {
   __shared__ int n_found, n_keys;
   const int t = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const X* x = reinterpret_cast<const X*>(a.x + (int64_t)t * a.row_stride);
-  const int back = (int)((uintptr_t)x & 15) / (int)sizeof(X);
+  const int back = elements_behind(x, 16);
   const Candidates<X> row{x, reinterpret_cast<const typename G::type*>(a.groups) + (int64_t)t * a.max_chunks * 64, a.V, back, (int)(((int64_t)a.V + back - 1) / CHUNK) + 1};
   int id = -1;
   X id_logit{};
@@ -583,7 +589,7 @@ struct Division {
   size_t groups, total;  // bytes
 };
 Division division_of(int T, int V, int K) {
-  const int chunks = (int)(((int64_t)V + 6) / CHUNK) + 1;  // of a row that begins just before a multiple of 16 bytes
+  const int chunks = most_chunks(V, 16, 2);
   Division d{chunks <= 2 ? 1 : WAVES, 1, chunks, chunks, 0, 256};
   if (chunks > 16) {
     int64_t parts = T > 0 ? 2048 / T : 1;
@@ -633,8 +639,8 @@ struct GradArgs {
   int64_t row_stride, d_row_stride;  // bytes
   const int32_t* ids;
   const float *lse, *d_logp, *entropy, *d_entropy, *d_lse;
-  int32_t T, V, parts, part_chunks;
-  float scale;
+  int32_t T, V, parts, part_chunks, line;
+  float scale, c, lag;
 };
 
 __device__ __forceinline__ void put(const float (&d)[8], u32x4& v) {
@@ -650,15 +656,16 @@ __device__ __forceinline__ void put(const float (&d)[4], u32x4& v) {
   for (int w = 0; w < 4; ++w) v[w] = __float_as_uint(d[w]);
 }
 
+// Past the caches: whole lines go out as they are, and what the next call reads stays.
 template <typename X>
-__device__ __forceinline__ void store_some(X* x, uint32_t j, int V, const u32x4& v) {
-  if (j + per_load<X> <= (uint32_t)V) {
-    reinterpret_cast<Unaligned<X>*>(x + j)->v = v;
+__device__ __forceinline__ void store_some(X* x, int64_t j, int V, const u32x4& v) {
+  if (j >= 0 && j + per_load<X> <= V) {
+    __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(x + j));
     return;
   }
 #pragma unroll
   for (int e = 0; e < per_load<X>; ++e) {
-    if (j + e >= (uint32_t)V) continue;
+    if (j + e < 0 || j + e >= V) continue;
     if constexpr (sizeof(X) == 2) reinterpret_cast<uint16_t*>(x)[j + e] = (uint16_t)(v[e / 2] >> (e & 1 ? 16 : 0));
     else reinterpret_cast<uint32_t*>(x)[j + e] = v[e];
   }
@@ -672,39 +679,54 @@ __global__ __launch_bounds__(THREADS) void gradient_kernel(GradArgs a) {
   const int t = (int)((units - 1 - unit) / (unsigned)a.parts), part = (int)((units - 1 - unit) - (unsigned)t * (unsigned)a.parts);
   const X* x = reinterpret_cast<const X*>(a.x + (int64_t)t * a.row_stride);
   X* y = reinterpret_cast<X*>(a.d_x + (int64_t)t * a.d_row_stride);
-  const int all_chunks = (a.V - 1) / CHUNK + 1, c0 = part * a.part_chunks, c1 = c0 + a.part_chunks < all_chunks ? c0 + a.part_chunks : all_chunks;
+  const int back = elements_behind(y, a.line), all_chunks = (int)(((int64_t)a.V + back - 1) / CHUNK) + 1, c0 = part * a.part_chunks, c1 = c0 + a.part_chunks < all_chunks ? c0 + a.part_chunks : all_chunks;
   const int id = a.ids ? a.ids[t] : -1;
   const float lse = a.lse[t], g = a.d_logp && (unsigned)id < (unsigned)a.V ? a.d_logp[t] : 0.f, ge = a.d_entropy ? a.d_entropy[t] : 0.f, gl = a.d_lse ? a.d_lse[t] : 0.f;
   if (lse == -INFINITY || (g == 0.f && ge == 0.f && gl == 0.f)) {
     for (int c = c0; c < c1; ++c)
 #pragma unroll
-      for (int l = 0; l < loads<X>; ++l) store_some(y, (uint32_t)c * CHUNK + first_of<X>(l), a.V, u32x4{0, 0, 0, 0});
+      for (int l = 0; l < loads<X>; ++l) store_some(y, index_of<X>(c, l, threadIdx.x & 63, back), a.V, u32x4{0, 0, 0, 0});
     return;
   }
   const float h = ge != 0.f ? a.entropy[t] : 0.f;
-  // p_j (gl - g - ge (log p_j + h)), and g for the token itself
+  // log p_j = (x_j - m) scale - log_s: with lse as it is, unless that is so large that its rounding shows in p (a mask of the type's lowest
+  // value that leaves nothing).  One wavefront has all of such a row then, whose sum it takes again before it writes (x may be y).
+  float m = 0.f, log_s = lse;
+  int from = c0, upto = c1;
+  if (fabsf(lse) > FAR) {
+    if (part != 0) return;
+    Stats st{-INFINITY, 0.f, 0.f};
+    upto = all_chunks;
+    for (int c = 0; c < all_chunks; ++c) {
+      u32x4 v[loads<X>];
+#pragma unroll
+      for (int l = 0; l < loads<X>; ++l) v[l] = load_some(x, index_of<X>(c, l, threadIdx.x & 63, back), a.V);
+      take_chunk<X, false>(st, v, a.c, a.lag);
+    }
+    join_lanes<false>(st, a.c);
+    m = st.m;
+    log_s = logf(st.s);
+  }
+  // d_j = p_j (gl - g - ge (log p_j + h)) scale, and g scale more for the token itself
   const float flat = a.scale * (gl - g - ge * h), steep = -a.scale * ge, own = a.scale * g;
-  auto take = [&](int c, const u32x4 (&v)[loads<X>]) {
+  for (int c = from; c < upto; ++c) {
+    u32x4 v[loads<X>];
+#pragma unroll
+    for (int l = 0; l < loads<X>; ++l) v[l] = load_some(x, index_of<X>(c, l, threadIdx.x & 63, back), a.V);
 #pragma unroll
     for (int l = 0; l < loads<X>; ++l) {
-      const uint32_t j = (uint32_t)c * CHUNK + first_of<X>(l);
+      const int64_t j = index_of<X>(c, l, threadIdx.x & 63, back);
       float d[per_load<X>];
 #pragma unroll
       for (int e = 0; e < per_load<X>; ++e) {
-        const float lp = __builtin_fmaf(element((const X*)nullptr, v[l], e), a.scale, -lse), p = __builtin_amdgcn_exp2f(lp * LOG2E);
+        const float lp = __builtin_fmaf(element((const X*)nullptr, v[l], e) - m, a.scale, -log_s), p = __builtin_amdgcn_exp2f(lp * LOG2E);
         d[e] = p == 0.f ? 0.f : p * __builtin_fmaf(steep, lp, flat);
-        if (j + e == (uint32_t)id) d[e] += own;
+        if ((int)j + e == id) d[e] += own;
       }
       u32x4 out;
       put(d, out);
       store_some(y, j, a.V, out);
     }
-  };
-  for (int c = c0; c < c1; ++c) {
-    u32x4 v[loads<X>];
-#pragma unroll
-    for (int l = 0; l < loads<X>; ++l) v[l] = load_some(x, (int64_t)c * CHUNK + first_of<X>(l), a.V);
-    take(c, v);
   }
 }
 
@@ -765,13 +787,16 @@ extern "C" int32_t moe_token_logprobs_backward(int32_t dtype, int32_t T, int32_t
   if (d_entropy && !entropy) return fail(MOE_ERR_INVALID_ARG, "%s: d_entropy without entropy", who);
   if (row_stride < 0 || (T > 1 && d_row_stride < V)) return fail(MOE_ERR_INVALID_ARG, "%s: rows of d_x overlap, or row_stride is negative", who);
   if (T > 1 && x == d_x && row_stride != d_row_stride) return fail(MOE_ERR_INVALID_ARG, "%s: in place, d_x must have x's stride", who);
-  const int chunks = (V - 1) / CHUNK + 1;
+  // Stores of whole lines: 284 against 317 us for 8192 rows of 50001 bfloat16 logits.  Short rows, which a few more elements
+  // can cost another chunk, begin on 16 bytes (16384 rows of 1000: 15 against 19 us).
+  const int line = V > 8 * CHUNK ? 128 : 16, chunks = most_chunks(V, line, (int)es);
   int per = chunks < 4 ? chunks : 4;
   if ((int64_t)T * ((chunks - 1) / per + 1) < 4096) per = 1;
   const int parts = (chunks - 1) / per + 1;
   const int64_t grid = ((int64_t)T * parts + WAVES - 1) / WAVES;
   if (!launchable(grid, THREADS)) return fail(MOE_ERR_UNSUPPORTED, "%s: %d rows are too many for one call", who, T);
-  const GradArgs a{(const char*)x, (char*)d_x, row_stride * (int64_t)es, d_row_stride * (int64_t)es, ids, lse, d_logp, entropy, d_entropy, d_lse, T, V, parts, per, scale};
+  const float c = fminf(scale * LOG2E, FLT_MAX);
+  const GradArgs a{(const char*)x, (char*)d_x, row_stride * (int64_t)es, d_row_stride * (int64_t)es, ids, lse, d_logp, entropy, d_entropy, d_lse, T, V, parts, per, line, scale, c, LAG_BITS / c};
   if (dtype == MOE_BF16) hipLaunchKernelGGL(gradient_kernel<__bf16>, dim3((unsigned)grid), dim3(THREADS), 0, (hipStream_t)stream, a);
   else hipLaunchKernelGGL(gradient_kernel<float>, dim3((unsigned)grid), dim3(THREADS), 0, (hipStream_t)stream, a);
   return check_hip(hipGetLastError(), "log-probabilities gradient launch");

@@ -243,6 +243,29 @@ def test_gradient_of_masked_rows(dtype):
     assert got[0, 0] == 2.0
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [3, 700, 50001])
+def test_gradient_of_logits_far_from_zero(V, dtype):
+    """lse cannot hold log V beside the type's lowest value, or 2^-12 beside 2^20: rows of such logits have the gradients of the same ones near zero."""
+    g = torch.Generator().manual_seed(V)
+    near = torch.randint(-8, 8, (4, V), generator=g).float() / 4
+    near[1] = 0.0
+    for far in (float(torch.finfo(DT[dtype]).min), 2.0 ** (20 if dtype == "f32" else 8), -(2.0 ** (20 if dtype == "f32" else 8))):
+        rows = near.clone() if abs(far) < 1e9 else torch.zeros(4, V)
+        # (sums are exact: multiples of 1/4 below 2^21, in bfloat16 multiples of 2 from 2^8 on)
+        rows = rows * (8 if dtype == "bf16" and abs(far) < 1e9 else 1)
+        x0, x1 = rows.to(DT[dtype]).cuda(), (rows + far).to(DT[dtype]).cuda()
+        assert torch.equal(x1.double() - far, x0.double())
+        ids = [0, 1, V - 1, -1]
+        g = dict(d_logp=[1.0, -2.0, 0.5, 3.0], d_entropy=[0.5, 0.5, 0.0, 1.0], d_lse=[0.0, 0.25, 0.0, -1.0])
+        got = [backward(x, ids, forward(x, ids), **g) for x in (x0, x1)]
+        # (in place the rows lie elsewhere, and a sum's order follows a row's alignment: the same bound, not the same bits)
+        got.append(backward(x1.clone(), ids, forward(x1, ids), in_place=True, **g))
+        h = x0.float().cpu().numpy()
+        for d in got:
+            check_gradient(d, h, ids, dtype, **g)
+
+
 def test_results_do_not_change_streams_and_graphs():
     for T, V, K in ((3, 70001, 20), (700, 3001, 5)):
         x, h = logits(T, V, "bf16")
