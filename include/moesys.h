@@ -689,8 +689,9 @@ int32_t moe_kv_release(const moe_kv_cache* c, int32_t* refs, const int32_t* lens
 
 /* Sequence dst[i] becomes another of the length and contents of sequence src[i], i < n <= n_seqs (device int32 [n]): it gives back its
  * pages, shares src's whole ones, and has a page of its own with a copy of the places in src's last, begun one;
- * lens[dst[i]] = lens[src[i]] (device int32 [n_seqs]).  No sequence may be dst twice, or src and dst; a pair outside
- * 0..n_seqs-1 or of one sequence is left out.  Where the page is not to be had, the places of the begun page are not there.
+ * lens[dst[i]] = lens[src[i]] (device int32 [n_seqs]).  A pair outside 0..n_seqs-1 or of one sequence is left out, and of the others
+ * those whose dst is some pair's src, or the dst of an earlier one.  Where the page is not to be had, the places of the begun page are
+ * not there.
  * ws: moe_kv_pages_workspace_bytes, 256-byte aligned, need not be cleared. */
 size_t moe_kv_pages_workspace_bytes(const moe_kv_cache* c);
 int32_t moe_kv_fork(const moe_kv_cache* c, int32_t* refs, int32_t n, const int32_t* src, const int32_t* dst, int32_t* lens,

@@ -117,6 +117,8 @@ class Pages:
         """Copies to make, (page, page, places), and how many pages were not to be had; lens follows."""
         S, copies, missing = len(self.table), [], 0
         pairs = [(int(a), int(b)) for a, b in zip(src, dst) if 0 <= a < S and 0 <= b < S and a != b]
+        sources, taken = {a for a, _ in pairs}, set()
+        pairs = [(a, b) for a, b in pairs if b not in sources and not (b in taken or taken.add(b))]
         size = lambda s: min(max(int(lens[s]), 0), len(self.table[s]) * self.P)  # noqa: E731
         for a, b in pairs:
             self.drop(b, 0)

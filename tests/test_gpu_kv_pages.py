@@ -146,6 +146,21 @@ def test_forks_that_are_left_out():
     pool.fork([], [], lens)
 
 
+@pytest.mark.parametrize("S,width", [(7, 6), (5000, 9)])
+def test_forks_into_one_sequence_or_from_one_that_is_written(S, width):
+    """Of the pairs of one dst the first is taken, and none whose dst is a src: few sequences and more than one workgroup holds."""
+    pool = Pool(S, width, S * 3 + 80, 16, hkv=1, D=8)
+    lens = [20 + s % 7 for s in range(S)]
+    lens[0] = 90
+    pool.reserve(lens)
+    lens = pool.fork([0, 1, 0, 3, 4, 9999], [2, 2, 2, 4, 5, 6], lens)     # 1 -> 2 and 0 -> 2 again, 3 -> 4 while 4 -> 5
+    assert lens[2] == 90 and lens[4] == 20 + 4 and lens[5] == 24
+    lens = pool.fork([0, 1, 2], [1, 2, 0], lens)                          # a ring: none of them
+    pool.reserve(lens, more=16)
+    pool.release(lens)
+    pool.fork([], [], lens)
+
+
 def test_entries_that_name_no_page():
     pool = Pool(4, 6, 30, 16)
     lens = [90, 50, 70, 0]
