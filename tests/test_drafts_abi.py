@@ -74,6 +74,14 @@ def test_oracle_pages():
     assert p.reserve([16, 9, -1], 5) == 1 and p.table[0] == [0, 2, 3, 5] and p.reserve([-1, 16, -1], 0) == 1 and p.table[1] == [0, 1, 4, -1]
 
 
+def test_oracle_forks_that_are_left_out():
+    p = O.Pages(np.full((5, 3), -1), np.zeros(20), 4)
+    lens = [9, 5, 2, 7, 1]
+    p.reserve(lens, 0)
+    p.fork([0, 1, 2, 4], [3, 3, 4, 0], lens)          # 3 twice; 4 and 0 are sources
+    assert lens == [9, 5, 2, 9, 1] and p.consistent() and p.table[3][:2] == p.table[0][:2]
+
+
 def test_oracle_compact_reads_before_it_writes():
     k = np.arange(6 * 4 * 2 * 8, dtype=float).reshape(6, 4, 2, 8)
     table = np.array([[3, 0, 4], [5, -1, 2]])
@@ -152,7 +160,7 @@ def test_pages_refuse():
         kw = {**dict(base=FAKE, width=4, keep=2 * FAKE, new=None), **bad}
         assert L.moe_kv_compact(ref(c), kw["base"], kw["width"], kw["keep"], kw["new"], None) == 1, bad
     assert L.moe_kv_compact(ref(cache(n_seqs=0)), None, 4, None, None, None) == 0
-    assert L.moe_kv_compact(ref(cache(n_seqs=2 ** 23, n_kv_heads=2)), FAKE, 4, 2 * FAKE, None, None) == 2
+    assert L.moe_kv_compact(ref(cache(n_seqs=2 ** 24, n_kv_heads=2)), FAKE, 4, 2 * FAKE, None, None) == 2
     assert L.moe_kv_release(ref(c), None, FAKE, None) == 1 and L.moe_kv_release(ref(c), FAKE, None, None) == 1
     assert L.moe_kv_release(ref(cache(n_seqs=0)), FAKE, None, None) == 0
 
