@@ -763,10 +763,10 @@ extern "C" int32_t moe_token_logprobs(int32_t dtype, int32_t T, int32_t V, const
   if (row_stride < 0) return fail(MOE_ERR_INVALID_ARG, "moe_token_logprobs: row_stride is negative");
   if (logp && !ids) return fail(MOE_ERR_INVALID_ARG, "moe_token_logprobs: logp without ids");
   if (K > 0 && (!top_ids || !top_logp)) return fail(MOE_ERR_INVALID_ARG, "moe_token_logprobs: top_ids and top_logp must both be given");
-  if (!ws || ((uintptr_t)ws & 255) || ws_bytes < need)
-    return fail(MOE_ERR_WORKSPACE, "moe_token_logprobs: workspace NULL, misaligned or smaller than %zu bytes", need);
   const Division d = division_of(T, V, K);
   if (!launchable((int64_t)T * d.parts, THREADS)) return fail(MOE_ERR_UNSUPPORTED, "moe_token_logprobs: %d rows are too many for one call", T);
+  if (!ws || ((uintptr_t)ws & 255) || ws_bytes < need)
+    return fail(MOE_ERR_WORKSPACE, "moe_token_logprobs: workspace NULL, misaligned or smaller than %zu bytes", need);
   const float c = fminf(scale * LOG2E, FLT_MAX);
   const RowArgs a{(const char*)x, row_stride * (int64_t)es, ids, logp, lse, entropy, top_logp, top_ids, (f32x4*)ws, (char*)ws + d.groups, T, V, K, d.parts, d.part_chunks, d.max_chunks, scale, c, LAG_BITS / c};
   return dtype == MOE_BF16 ? launch_rows<__bf16>(a, d, (hipStream_t)stream) : launch_rows<float>(a, d, (hipStream_t)stream);
