@@ -12,51 +12,12 @@
 //    places of an instruction are taken in that order.  The first operand pairs the halves of the values of two places.
 //  - The queries of all rows lie in LDS, 16 bytes of padding to a row: every wavefront reads all of them for each tile.
 //  - Who sees what is looked up only in tiles that hold new tokens, a window's edge or places that are not there.
-#include "attention_internal.h"
-#include "draft_tokens.h"
-#include "wave_util.h"
-#include <float.h>
-#include <math.h>
-#include <type_traits>
+#include "tree_parts.h"
 
 namespace moesys {
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef short i16x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-
-constexpr int WAVES = 4;
-constexpr int LEAST = 2 * WAVES;     // tiles of a part, at least
-constexpr int SMALL_PLACES = 1024;   // sequences up to this length are not split where there is a workgroup for each
-// How far a score may pass the running maximum before the maximum moves (a little less than 8 log 2); weights are scaled down by 2^8.
-constexpr int LAG_BITS = 8;
-constexpr float LAG = 5.5f;
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-
-// Rows of places that are not there and dimensions beyond head_dim are read from here.
-__device__ const u32x4 ZEROS[MOE_MAX_HEAD_DIM * 4 / 16] = {};
-
-struct TreeArgs {
-  const char *k, *v, *q;
-  char* out;
-  float* lse;
-  const int32_t *table, *lens, *first;
-  const uint64_t* words;
-  const float* slopes;
-  float* part_o;   // [slot][items][rows][D]
-  f32x2* part_ml;  // [slot][items][rows]
-  int2* plan;      // [row tile][sequence]: slot of the first piece, pieces
-  int64_t n_pages, page_stride, token_stride, head_stride, q_token, q_head, o_token, o_head;  // bytes
-  PageDivisor page, per_head, group;  // places of a page, items of a kv head, query heads of a kv head
-  double inverse_parts;
-  int32_t page_size, table_width, capacity, n_seqs, hq, G, T, max_new, D, window, sinks, rows, items, row_tiles, parts, may_split;
-  float scale, cap, inv_cap;
-};
+constexpr int LEAST = 2 * WAVES;  // tiles of a part, at least
 
 template <typename X, int DP> struct Shape;
 template <int DP> struct Shape<__bf16, DP> {
@@ -71,89 +32,6 @@ template <> struct Words<16> { typedef u32x4 type; };
 
 // Workgroups that a CU holds.
 constexpr int resident_workgroups(int dims, int elem, int blocks) { return blocks * dims <= 256 && dims * elem < 1024 ? 2 : 1; }
-
-__device__ __forceinline__ Drafts drafts(const TreeArgs& a, int s) { return drafts_of(a.first[s], a.first[s + 1], a.T, a.max_new, a.lens[s], a.capacity); }
-
-// A value that all lanes hold, for the scalar registers.
-__device__ __forceinline__ int64_t uniform(int64_t v, int lane) {
-  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)v, lane), hi = __builtin_amdgcn_readlane((int)(v >> 32), lane);
-  return (int64_t)(((uint64_t)hi << 32) | lo);
-}
-
-// How the workgroups of an item share the batch: its sequences' tiles stand in one row, of which part w has w*share .. (w+1)*share - 1.
-struct Deal {
-  int64_t share, total, begin;  // of a part, of the row; where in the row sequence b begins
-  int b;                        // the part's first sequence
-  bool one_each;                // the row counts sequences, none is split
-};
-
-// Places in the row of sequence s, whose row tile rt may have no rows.
-template <int TILE>
-__device__ __forceinline__ int places_in_row(const TreeArgs& a, int s, int rt, int& tiles) {
-  const Drafts d = drafts(a, s);
-  tiles = span_of(d, a.window, a.sinks, TILE).tiles;
-  return rt * a.rows < d.n * a.G ? (int)row_tiles(tiles) : 0;
-}
-
-template <int TILE>
-__device__ __forceinline__ Deal deal(const TreeArgs& a, int rt, int w) {
-  const int lane = threadIdx.x & 63;
-  Deal p{};
-  if (!a.may_split) {
-    p.one_each = true;
-    p.share = share_of_row(a.n_seqs, a.inverse_parts, 1);
-    p.total = a.n_seqs;
-    p.begin = w * p.share;
-    p.b = (int)p.begin;
-    return p;
-  }
-  int longest = 0, tiles = 0;
-  int64_t total = 0, mine0 = 0;
-  for (int s = lane; s < a.n_seqs; s += 64) {
-    const int mine = places_in_row<TILE>(a, s, rt, tiles);
-    if (s == lane) mine0 = mine;
-    total += mine;
-    longest = tiles > longest ? tiles : longest;
-  }
-  if (a.n_seqs <= a.parts && !__any(longest > SMALL_PLACES / TILE)) {
-    p.one_each = true;
-    p.share = 1;
-    p.total = a.n_seqs;
-    p.begin = p.b = w;
-    return p;
-  }
-  for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d, 64);
-  p.total = uniform(total, 0);
-  p.share = uniform(share_of_row(p.total, a.inverse_parts, LEAST), 0);
-  const int64_t at = w * p.share;
-  int64_t mine = mine0;
-  for (int s = 0; s < a.n_seqs; s += 64) {
-    if (s) mine = s + lane < a.n_seqs ? places_in_row<TILE>(a, s + lane, rt, tiles) : 0;
-    int64_t upto = mine;
-    for (int d = 1; d < 64; d <<= 1) {
-      const int64_t other = __shfl_up(upto, d, 64);
-      if (lane >= d) upto += other;
-    }
-    const unsigned long long beyond = __ballot(p.begin + upto > at);
-    if (beyond) {
-      const int who = __ffsll(beyond) - 1;
-      p.b = s + who;
-      p.begin += uniform(upto - mine, who);
-      return p;
-    }
-    p.begin += uniform(upto, 63);
-  }
-  p.total = 0;  // nothing is left for this part
-  return p;
-}
-
-// exp(x), the last step a power of two
-__device__ __forceinline__ float power(float x) { return __builtin_amdgcn_exp2f(x * LOG2E); }
-
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  const bf16x2 v = {(__bf16)lo, (__bf16)hi};
-  return __builtin_bit_cast(uint32_t, v);
-}
 
 // Addresses that come out of LDS are global ones: told so, the compiler reads them with loads that the waits for LDS do not wait for.
 template <bool NT, typename W>
@@ -195,23 +73,6 @@ __device__ __forceinline__ void half_lines(u32x4& a, u32x4& b) {
   }
 }
 
-// Of a pair of bfloat16 numbers, those that are infinite or NaN: 1.0 in their place, 0 elsewhere.
-__device__ __forceinline__ uint32_t not_finite(uint32_t v) {
-  return ((v & 0x7f80u) == 0x7f80u ? 0x3f80u : 0u) | ((v & 0x7f800000u) == 0x7f800000u ? 0x3f800000u : 0u);
-}
-__device__ __forceinline__ float not_finite(float v) { return fabsf(v) < INFINITY ? 0.f : 1.f; }
-
-// Four finished elements of a row; the first four bring the row's lse along.
-template <typename X>
-__device__ __forceinline__ void store_row(const TreeArgs& a, int t, int h, int d, f32x4 y, float sum, float top) {
-  if (sum == 0.f) y = f32x4{0.f, 0.f, 0.f, 0.f};
-  else y *= 1.f / sum;
-  char* p = a.out + (int64_t)t * a.o_token + (int64_t)h * a.o_head + d * sizeof(X);
-  if constexpr (sizeof(X) == 2) *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
-  else *reinterpret_cast<f32x4*>(p) = y;
-  if (a.lse && d == 0) a.lse[(int64_t)t * a.hq + h] = sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum * (1 << LAG_BITS)) * LN2;
-}
-
 // A part of the batch per workgroup, piece after piece; its wavefronts take an item's tiles in turn.  An item is a kv head and up
 // to 16 RB of the rows that its tokens and query heads make.
 // FULL: head_dim is DP, no lane's dimensions lie beyond it.
@@ -233,8 +94,8 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X), RB))
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m16 = lane & 15, g = lane >> 4, line_at = (g + 4 * (m16 >> 3)) * 16;
-  const int w = blockIdx.x / a.items, item = blockIdx.x - w * a.items, hk = a.per_head.quotient(item), rt = item - hk * a.row_tiles;
-  Deal at = deal<TILE>(a, rt, w);
+  const int w = blockIdx.x / a.items, item = blockIdx.x - w * a.items, rt = a.kv_heads.quotient(item), hk = item - rt * a.hkv;
+  Deal at = deal<TILE, LEAST>(a, rt, w);
   int64_t x = w * at.share;
   const int64_t x_end = x + at.share < at.total ? x + at.share : at.total;
   if (x >= x_end) return;
@@ -624,7 +485,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(TreeArgs a) {
   if (s >= a.n_seqs) return;
   const Drafts d = drafts(a, s);
   if (i >= d.n) return;
-  const int hk = a.group.quotient(h), rr = i * a.G + h - hk * a.G, rt = rr / a.rows, r = rr - rt * a.rows, item = hk * a.row_tiles + rt;
+  const int hk = a.group.quotient(h), rr = i * a.G + h - hk * a.G, rt = rr / a.rows, r = rr - rt * a.rows, item = rt * a.hkv + hk;
   const int2 plan = a.plan[(int64_t)rt * a.n_seqs + s];
   if (plan.y <= 1) return;
   auto row = [&](int j) { return ((int64_t)piece_slot(plan.x, j) * a.items + item) * a.rows + r; };
@@ -660,24 +521,25 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(TreeArgs a) {
 // The split of a call: what its grid, its workspace and its kernels agree on.
 struct Split {
   int blocks, rows, row_tiles, items, parts;
-  bool nt, may_split;
+  bool shared, nt, may_split;
   size_t ml, o, total;  // bytes: offsets of the pieces (the plan lies in front)
 };
 
 Split split_of(const moe_kv_cache* c, int32_t n_q_heads, int32_t max_new, int32_t window, int32_t sinks) {
   Split s;
   const int es = (int)elem_size(c->dtype), rows = max_new * (n_q_heads / c->n_kv_heads), dims = c->head_dim <= 64 ? 64 : c->head_dim <= 128 ? 128 : 256;
-  s.blocks = rows <= 16 ? 1 : rows <= 32 || es == 4 || dims > 128 ? 2 : 4;
-  s.rows = 16 * s.blocks;
+  s.shared = es == 2 && rows > SHARED_FROM;
+  s.blocks = s.shared ? shared_blocks(rows, dims) : rows <= 16 ? 1 : 2;
+  s.rows = 16 * s.blocks * (s.shared ? WAVES : 1);
   s.row_tiles = (rows + s.rows - 1) / s.rows;
   s.items = c->n_kv_heads * s.row_tiles;
   const int64_t capacity = (int64_t)c->table_width * c->page_size, reach = (int64_t)window + sinks + MOE_MAX_DRAFTS + 64;
   const int64_t kept = window > 0 && reach < capacity ? reach : capacity;
   s.may_split = kept > SMALL_PLACES;
-  const int64_t resident = 256 * resident_workgroups(dims, es, s.blocks);
+  const int64_t resident = 256 * (s.shared ? 2 : resident_workgroups(dims, es, s.blocks));
   int64_t parts = resident / s.items > 1 ? resident / s.items : 1;
-  const int tile = es == 2 && dims <= 128 ? 32 : 16;
-  const int64_t most = (int64_t)c->n_seqs * ((capacity + tile * LEAST - 1) / (tile * LEAST));  // pieces of work there can be
+  const int least = s.shared ? shared_tile(dims) * shared_least(dims) : (es == 2 && dims <= 128 ? 32 : 16) * LEAST;  // places of a part
+  const int64_t most = (int64_t)c->n_seqs * ((capacity + least - 1) / least);  // pieces of work there can be
   if (parts > most) parts = most > 1 ? most : 1;
   if (!s.may_split) parts = c->n_seqs;
   s.parts = (int)parts;
@@ -704,14 +566,16 @@ void launch(const TreeArgs& a, int blocks, unsigned grid, bool nt, hipStream_t s
     else launch<X, DP, decltype(rb)::value, false>(a, grid, nt, s);
   };
   if (blocks == 1) of(std::integral_constant<int, 1>());
-  else if (blocks == 2) of(std::integral_constant<int, 2>());
-  else if constexpr (sizeof(X) == 2 && DP <= 128) of(std::integral_constant<int, 4>());
+  else of(std::integral_constant<int, 2>());
 }
 
 template <typename X>
 int32_t launch_tree(const TreeArgs& a, const Split& sp, hipStream_t s) {
   const unsigned grid = (unsigned)((int64_t)sp.parts * sp.items);
-  if (a.D <= 64) launch<X, 64>(a, sp.blocks, grid, sp.nt, s);
+  if (sp.shared) {
+    const int32_t st = launch_tree_shared(a, sp.blocks, grid, sp.nt, s);
+    if (st != MOE_OK) return st;
+  } else if (a.D <= 64) launch<X, 64>(a, sp.blocks, grid, sp.nt, s);
   else if (a.D <= 128) launch<X, 128>(a, sp.blocks, grid, sp.nt, s);
   else launch<X, 256>(a, sp.blocks, grid, sp.nt, s);
   const int32_t st = check_hip(hipGetLastError(), "tree attention launch");
@@ -802,7 +666,8 @@ extern "C" int32_t moe_attention_tree(const moe_kv_cache* c, int32_t n_q_heads, 
   a.sinks = opt->sinks;
   a.rows = sp.rows;
   a.row_tiles = sp.row_tiles;
-  a.per_head = page_divisor(sp.row_tiles);
+  a.kv_heads = page_divisor(c->n_kv_heads);
+  a.hkv = c->n_kv_heads;
   a.items = sp.items;
   a.parts = sp.parts;
   a.inverse_parts = 1.0 / sp.parts;
