@@ -520,7 +520,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(TreeArgs a) {
 
 // The split of a call: what its grid, its workspace and its kernels agree on.
 struct Split {
-  int blocks, rows, row_tiles, items, parts;
+  int blocks, rows, row_tiles, items, parts, small;
   bool shared, nt, may_split;
   size_t ml, o, total;  // bytes: offsets of the pieces (the plan lies in front)
 };
@@ -535,10 +535,13 @@ Split split_of(const moe_kv_cache* c, int32_t n_q_heads, int32_t max_new, int32_
   s.items = c->n_kv_heads * s.row_tiles;
   const int64_t capacity = (int64_t)c->table_width * c->page_size, reach = (int64_t)window + sinks + MOE_MAX_DRAFTS + 64;
   const int64_t kept = window > 0 && reach < capacity ? reach : capacity;
-  s.may_split = kept > SMALL_PLACES;
+  // A workgroup takes 128 or 64 places at a time where wavefronts have tiles of their own, 64 or 32 where they share them: 8 steps are
+  // about the time of the launch that joins pieces.
+  s.small = s.shared ? 256 : 1024;
+  s.may_split = kept > s.small;
   const int64_t resident = 256 * (s.shared ? 2 : resident_workgroups(dims, es, s.blocks));
   int64_t parts = resident / s.items > 1 ? resident / s.items : 1;
-  const int least = s.shared ? shared_tile(dims) * shared_least(dims) : (es == 2 && dims <= 128 ? 32 : 16) * LEAST;  // places of a part
+  const int least = s.shared ? 256 : (es == 2 && dims <= 128 ? 32 : 16) * LEAST;  // places of a part
   const int64_t most = (int64_t)c->n_seqs * ((capacity + least - 1) / least);  // pieces of work there can be
   if (parts > most) parts = most > 1 ? most : 1;
   if (!s.may_split) parts = c->n_seqs;
@@ -672,6 +675,7 @@ extern "C" int32_t moe_attention_tree(const moe_kv_cache* c, int32_t n_q_heads, 
   a.parts = sp.parts;
   a.inverse_parts = 1.0 / sp.parts;
   a.may_split = sp.may_split;
+  a.small = sp.small;
   a.scale = opt->scale;
   a.cap = opt->softcap;
   // (finite for the smallest caps too: a score of 0 stays 0)

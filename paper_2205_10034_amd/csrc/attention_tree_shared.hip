@@ -34,11 +34,12 @@ __device__ __forceinline__ u32x4 read16(const char* p) {
   else return *at;
 }
 
-// FULL: head_dim is DP.  A wavefront has 16 RB rows of the workgroup's.
-template <int DP, int RB, bool FULL, bool NT>
+// FULL: head_dim is DP.  PLAIN: no cap, no slopes.  A wavefront has 16 RB rows of the workgroup's.
+template <int DP, int RB, bool FULL, bool NT, bool PLAIN>
 __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
-  constexpr int TILE = shared_tile(DP), SUB = TILE / 16, PAIRS = SUB / 2, KSTEPS = DP / 32, NDB = DP / 16, PITCH = 2 * DP;
+  constexpr int TILE = shared_tile(DP, RB), SUB = TILE / 16, PAIRS = SUB / 2, KSTEPS = DP / 32, NDB = DP / 16, PITCH = 2 * DP;
   constexpr int CHUNKS = DP / 8, ROWS = 16 * RB * WAVES, MINE = TILE / WAVES, PER = 64 / CHUNKS, LOADS = MINE / PER;
+  constexpr int SETS = RB == 1 && DP <= 128 ? 2 : 1;  // of registers for tiles on their way
   constexpr uint64_t EVERY = TILE == 64 ? ~0ull : (1ull << TILE) - 1;
   constexpr float LAG2 = LAG_BITS - 0.05f;
   __shared__ __attribute__((aligned(1024))) char tiles[2][2][TILE * PITCH];  // [buffer][keys, values]
@@ -48,16 +49,16 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m16 = lane & 15, g = lane >> 4;
   const int w = blockIdx.x / a.items, item = blockIdx.x - w * a.items, rt = a.kv_heads.quotient(item), hk = item - rt * a.hkv;
-  Deal at = deal<TILE, shared_least(DP)>(a, rt, w);
+  Deal at = deal<TILE, shared_least(DP, RB)>(a, rt, w);
   int64_t x = w * at.share;
   const int64_t x_end = x + at.share < at.total ? x + at.share : at.total;
   if (x >= x_end) return;
   const char* zeros = reinterpret_cast<const char*>(ZEROS);
-  const char *k_head = a.k + hk * a.head_stride, *v_head = a.v + hk * a.head_stride;
 
   // this lane's part of a tile: of its wavefront's rows MINE, row PER*i + lane / CHUNKS, one chunk
   const int my_row = lane / CHUNKS, my_chunk = lane % CHUNKS;
   const bool chunk_there = FULL || my_chunk * 8 < a.D;
+  const char *k_chunk = a.k + hk * a.head_stride + my_chunk * 16, *v_chunk = a.v + hk * a.head_stride + my_chunk * 16;
   int store_at[LOADS];
 #pragma unroll
   for (int i = 0; i < LOADS; ++i) {
@@ -68,7 +69,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
   const int key_at = m16 * PITCH + ((g ^ key_of<CHUNKS>(m16)) << 4);
   const int v_row = g * 4 + (m16 >> 2), value_at = v_row * PITCH + (((m16 >> 1 & 1) ^ key_of<CHUNKS>(v_row)) << 4) + (m16 & 1) * 8;
 
-  const bool plain = a.cap == 0.f && !a.slopes;
   const float c2 = a.scale * LOG2E;
 
   for (int piece_no = 0; x < x_end; ++piece_no) {
@@ -99,31 +99,48 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
       const int p = (int)((unsigned)span.tile(u) * TILE + wave * MINE + (lane & (MINE - 1))), page = u < upto && p < d.len ? valid_page(entry, a.n_pages) : -1;
       return page >= 0 ? page * a.page_stride + (p - a.page.quotient(p) * a.page_size) * a.token_stride : (int64_t)-1;
     };
-    u32x4 kr[LOADS], vr[LOADS];
-    uint32_t coming = 0;  // which of the wavefront's rows are there
-    auto load = [&](int64_t row) {
-      coming = (uint32_t)__ballot(row >= 0) & ((1u << MINE) - 1);
+    // Where this lane's rows of the tile that is loaded next lie, worked out a tile before: what the lanes tell one another takes as long as
+    // many products.
+    int64_t next[LOADS];
+    uint32_t next_there = 0, coming[SETS];  // which of the wavefront's rows are there; of those on their way
+    auto place = [&](int64_t row) {
+      next_there = (uint32_t)__ballot(row >= 0) & ((1u << MINE) - 1);
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {
         const int lo = __shfl((int)(uint32_t)row, i * PER + my_row, 64), hi = __shfl((int)(row >> 32), i * PER + my_row, 64);
-        const int64_t off = (int64_t)(((uint64_t)(uint32_t)hi << 32) | (uint32_t)lo);
-        const bool have = hi >= 0 && chunk_there;
-        kr[i] = read16<NT>(have ? k_head + off + my_chunk * 16 : zeros);
-        vr[i] = read16<NT>(have ? v_head + off + my_chunk * 16 : zeros);
+        next[i] = (int64_t)(((uint64_t)(uint32_t)hi << 32) | (uint32_t)lo);
       }
     };
-    auto put = [&](int buffer) {
+    u32x4 kr[SETS][LOADS], vr[SETS][LOADS];
+    auto load = [&](int set) {
+      coming[set] = next_there;
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {
-        *reinterpret_cast<u32x4*>(tiles[buffer][0] + store_at[i]) = kr[i];
-        *reinterpret_cast<u32x4*>(tiles[buffer][1] + store_at[i]) = vr[i];
+        const bool have = next[i] >= 0 && chunk_there;
+        kr[set][i] = read16<NT>(have ? k_chunk + next[i] : zeros);
+        vr[set][i] = read16<NT>(have ? v_chunk + next[i] : zeros);
       }
-      if (lane == 0) there[buffer][wave] = (uint16_t)coming;
+    };
+    auto put = [&](int set, int buffer) {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        *reinterpret_cast<u32x4*>(tiles[buffer][0] + store_at[i]) = kr[set][i];
+        *reinterpret_cast<u32x4*>(tiles[buffer][1] + store_at[i]) = vr[set][i];
+      }
+      if (lane == 0) there[buffer][wave] = (uint16_t)coming[set];
     };
 
     lds_barrier();  // (the piece before has been read)
     int entry = entry_of(from + 1);
-    load(row_of(from, entry_of(from)));
+    place(row_of(from, entry_of(from)));
+    load(0);
+    place(row_of(from + 1, entry));
+    entry = entry_of(from + 2);
+    if constexpr (SETS == 2) {
+      load(1);
+      place(row_of(from + 2, entry));
+      entry = entry_of(from + 3);
+    }
     auto sees = [&](int i) { return seen_drafts(a.words, a.words ? a.words[d.first + i] : 0, i, d.n); };
     if ((int)threadIdx.x < d.n) depth_lds[threadIdx.x] = draft_depth(sees(threadIdx.x), threadIdx.x);
     if ((int)threadIdx.x < ROWS) {
@@ -140,7 +157,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
 #pragma unroll
       for (int ks = 0; ks < KSTEPS; ++ks) q[rb][ks] = read16<false>(r < my_rows && (FULL || ks * 32 + g * 8 < a.D) ? from_q + ks * 64 : zeros);
     }
-    put(0);
+    put(0, 0);
     lds_barrier();
     int pos[RB];
     float slope[RB];
@@ -154,7 +171,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
 
     // Plain scores (no cap, no slopes) are taken as powers of two at once, exp2(c2 z - m), and m is in those units too; others, and those whose
     // powers would be beyond 2^100, keep their own units until the maximum is taken off.
-    bool fast = plain && a.scale > 0.f && c2 < 1e30f;
+    bool fast = PLAIN && a.scale > 0.f && c2 < 1e30f;
     float m[RB], l[RB];
     f32x4 o[RB][NDB];
 #pragma unroll
@@ -165,11 +182,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
       for (int db = 0; db < NDB; ++db) o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    auto compute = [&](int u, int buffer) {
-      const char *keys = tiles[buffer][0], *values = tiles[buffer][1];
-      uint64_t here = 0;
+    // Keys of two steps of the contraction index, values of AHEAD instructions are read before they are wanted: a read takes as long as four to eight
+    // of the matrix instructions that wait for it, and the compiler by itself keeps none of them ahead.
+    constexpr int AHEAD = RB == 1 ? 6 : 4, VALUES = PAIRS * NDB;
+    auto read_keys = [&](bf16x8 (&key)[2][SUB], int buffer, int ks) {
 #pragma unroll
-      for (int v = 0; v < WAVES; ++v) here |= (uint64_t)there[buffer][v] << (v * MINE);
+      for (int st = 0; st < SUB; ++st) key[ks & 1][st] = *reinterpret_cast<const bf16x8*>(tiles[buffer][0] + ((key_at ^ ks << 6) + st * 16 * PITCH));
+    };
+    auto read_values = [&](int buffer, int n) { return values_of(tiles[buffer][1] + ((value_at ^ (n % NDB) << 5) + n / NDB * 32 * PITCH), 16 * PITCH); };
+    auto compute = [&](int u, int buffer, uint64_t here, bf16x8 (&key)[2][SUB]) {
       const int p0 = span.tile(u) * TILE;
       f32x4 z[RB][SUB];
 #pragma unroll
@@ -177,15 +198,16 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
 #pragma unroll
         for (int st = 0; st < SUB; ++st) z[rb][st] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int ks = 0; ks < KSTEPS; ++ks)
+      for (int ks = 0; ks < KSTEPS; ++ks) {
 #pragma unroll
-        for (int st = 0; st < SUB; ++st) {
-          const bf16x8 key = *reinterpret_cast<const bf16x8*>(keys + ((key_at ^ ks << 6) + st * 16 * PITCH));
+        for (int st = 0; st < SUB; ++st)
 #pragma unroll
-          for (int rb = 0; rb < RB; ++rb) z[rb][st] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, __builtin_bit_cast(bf16x8, q[rb][ks]), z[rb][st], 0, 0, 0);
-        }
+          for (int rb = 0; rb < RB; ++rb) z[rb][st] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key[ks & 1][st], __builtin_bit_cast(bf16x8, q[rb][ks]), z[rb][st], 0, 0, 0);
+        if (ks + 2 < KSTEPS) read_keys(key, buffer, ks + 2);
+        __builtin_amdgcn_sched_barrier(0);
+      }
       const bool with_drafts = p0 + TILE > d.base;
-      if (!plain) {
+      if constexpr (!PLAIN) {
 #pragma unroll
         for (int st = 0; st < SUB; ++st)
 #pragma unroll
@@ -200,7 +222,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
               z[rb][st][i] = s - slope[rb] * (float)(pos[rb] - pos_p);
             }
           }
-      } else if (!fast) {
+      } else if (__builtin_expect(!fast, 0)) {
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
@@ -209,8 +231,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
       // Everyone sees everything of a tile that is all there, before the new tokens, and in the window of the last position or among
       // the sinks.
       const bool masked = here != EVERY || with_drafts || (a.window > 0 && last_pos - p0 >= a.window && p0 + TILE > a.sinks);
-      uint32_t seen_here[RB];  // places that this lane's rows see, 4 SUB bits
-      if (masked) {
+      uint32_t seen_here[RB] = {};  // places that this lane's rows see, 4 SUB bits
+      if (__builtin_expect(masked, 0)) {
         uint64_t seen[RB];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
@@ -247,7 +269,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
         if (fast) top[rb] *= c2;
         moves |= top[rb] > m[rb] + (fast ? LAG2 : LAG);
       }
-      if (__any(moves)) {
+      if (__builtin_expect(__any(moves), 0)) {
         bool far = false;
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
@@ -255,7 +277,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
           top[rb] = fmaxf(top[rb], __shfl_xor(top[rb], 32, 64));
           far |= fabsf(top[rb]) > 0x1p100f && top[rb] != -INFINITY;
         }
-        if (fast && __any(far)) {  // (as far from 0 as that, what the conversion rounds is either the same or gone)
+        if (__builtin_expect(fast && __any(far), 0)) {  // (as far from 0 as that, what the conversion rounds is either the same or gone)
           fast = false;
 #pragma unroll
           for (int rb = 0; rb < RB; ++rb) {
@@ -280,10 +302,27 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
           for (int db = 0; db < NDB; ++db) o[rb][db] *= f;
         }
       }
+      // A value that is not finite and that only some rows see would reach the others as 0 times it: it is left out of the product, and
+      // its element of the rows that see it becomes NaN.
+      bool odd = false;
+      if (__builtin_expect(masked, 0)) {
+        uint32_t any = 0;
+#pragma unroll
+        for (int n = 0; n < VALUES; ++n) {
+          const u32x4 bits = __builtin_bit_cast(u32x4, read_values(buffer, n));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) any |= not_finite(bits[i]);
+        }
+        odd = __any(any != 0);
+      }
+      bf16x8 value[AHEAD];
+#pragma unroll
+      for (int n = 0; n < AHEAD; ++n) value[n] = read_values(buffer, n);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
         const float ref = m[rb] == -INFINITY ? 0.f : m[rb];
-        if (fast) {
+        if (__builtin_expect(fast, 1)) {
           const float shift = -(ref + LAG_BITS);
 #pragma unroll
           for (int st = 0; st < SUB; ++st)
@@ -302,64 +341,82 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
       }
       // A weight enters as the sum of two bfloat16 numbers, each rounded to nearest: 17 bits of it, an error that half a step of the
       // output covers unless 2^8 values cancel.
+      u32x4 head[RB][PAIRS], rest[RB][PAIRS];
 #pragma unroll
-      for (int pr = 0; pr < PAIRS; ++pr) {
-        u32x4 head[RB], rest[RB];
+      for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb)
+        for (int pr = 0; pr < PAIRS; ++pr)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float w0 = z[rb][2 * pr + i / 2][i % 2 * 2], w1 = z[rb][2 * pr + i / 2][i % 2 * 2 + 1];
-            const uint32_t h = pack_bf16(w0, w1);
-            head[rb][i] = h;
-            rest[rb][i] = pack_bf16(w0 - __uint_as_float(h << 16), w1 - __uint_as_float(h & 0xffff0000u));
+            uint32_t h = pack_bf16(w0, w1);
+            asm("" : "+v"(h));  // (or each half is rounded once more by itself)
+            head[rb][pr][i] = h;
+            rest[rb][pr][i] = pack_bf16(w0 - __uint_as_float(h << 16), w1 - __uint_as_float(h & 0xffff0000u));
           }
+      // two blocks of dims at a time: four or more products between two of the same sum
 #pragma unroll
-        for (int db = 0; db < NDB; ++db) {
-          bf16x8 v = values_of(values + ((value_at ^ db << 5) + pr * 32 * PITCH), 16 * PITCH);
-          if (masked) {
-            // A value that is not finite and that only some rows see would reach the others as 0 times it: it is left out of the
-            // product, and its element of the rows that see it becomes NaN.
-            u32x4 bits = __builtin_bit_cast(u32x4, v), bad;
-            uint32_t any = 0;
+      for (int n0 = 0; n0 < VALUES; n0 += 2) {
+        if (__builtin_expect(odd, 0)) {  // (out of the way: a jump over it costs as much as two products)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) any |= bad[i] = not_finite(bits[i]);
-            if (__any(any != 0)) {
+          for (int n = n0; n < n0 + 2; ++n) {
+            u32x4 bits = __builtin_bit_cast(u32x4, value[n % AHEAD]), bad;
 #pragma unroll
-              for (int i = 0; i < 4; ++i) bits[i] &= ~((bad[i] & 0xffffu ? 0xffffu : 0u) | (bad[i] >> 16 ? 0xffff0000u : 0u));
-              v = __builtin_bit_cast(bf16x8, bits);
+            for (int i = 0; i < 4; ++i) {
+              bad[i] = not_finite(bits[i]);
+              bits[i] &= ~((bad[i] & 0xffffu ? 0xffffu : 0u) | (bad[i] >> 16 ? 0xffff0000u : 0u));
+            }
+            value[n % AHEAD] = __builtin_bit_cast(bf16x8, bits);
 #pragma unroll
-              for (int rb = 0; rb < RB; ++rb) {
-                u32x4 see;
+            for (int rb = 0; rb < RB; ++rb) {
+              u32x4 see;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  const uint32_t s = seen_here[rb] >> ((2 * pr + i / 2) * 4 + i % 2 * 2);
-                  see[i] = (s & 1 ? 0x3f80u : 0u) | (s & 2 ? 0x3f800000u : 0u);
-                }
-                const f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, bad), __builtin_bit_cast(bf16x8, see), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                  if (hit[i] > 0.f) o[rb][db][i] = NAN;
+              for (int i = 0; i < 4; ++i) {
+                const uint32_t s = seen_here[rb] >> ((2 * (n / NDB) + i / 2) * 4 + i % 2 * 2);
+                see[i] = (s & 1 ? 0x3f80u : 0u) | (s & 2 ? 0x3f800000u : 0u);
               }
+              const f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, bad), __builtin_bit_cast(bf16x8, see), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (hit[i] > 0.f) o[rb][n % NDB][i] = NAN;
             }
           }
-#pragma unroll
-          for (int rb = 0; rb < RB; ++rb) {
-            o[rb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8, head[rb]), o[rb][db], 0, 0, 0);
-            o[rb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8, rest[rb]), o[rb][db], 0, 0, 0);
-          }
         }
+#pragma unroll
+        for (int part = 0; part < 2; ++part)
+#pragma unroll
+          for (int n = n0; n < n0 + 2; ++n)
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+              o[rb][n % NDB] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value[n % AHEAD], __builtin_bit_cast(bf16x8, part == 0 ? head[rb][n / NDB] : rest[rb][n / NDB]), o[rb][n % NDB], 0, 0, 0);
+#pragma unroll
+        for (int n = n0; n < n0 + 2; ++n)
+          if (n + AHEAD < VALUES) value[n % AHEAD] = read_values(buffer, n + AHEAD);
+        __builtin_amdgcn_sched_barrier(0);
       }
     };
 
-    for (int u = from, buffer = 0; u < upto; ++u, buffer ^= 1) {
-      load(row_of(u + 1, entry));  // (of a tile behind the last one: zeros)
-      entry = entry_of(u + 2);
+    auto step = [&](int u, auto parity) __attribute__((always_inline)) {
+      constexpr int BUFFER = decltype(parity)::value;
+      bf16x8 key[2][SUB];
+      read_keys(key, BUFFER, 0);
+      read_keys(key, BUFFER, 1);
+      uint64_t here = 0;
+#pragma unroll
+      for (int v = 0; v < WAVES; ++v) here |= (uint64_t)there[BUFFER][v] << (v * MINE);
+      load(SETS == 2 ? BUFFER : 0);  // tile u + SETS (one behind the last one: zeros)
+      place(row_of(u + SETS + 1, entry));
+      entry = entry_of(u + SETS + 2);
       __builtin_amdgcn_sched_barrier(0);  // (they are on their way while the tile is worked on)
-      if (active) compute(u, buffer);
+      if (active) compute(u, BUFFER, here, key);
       __builtin_amdgcn_sched_barrier(0);
-      put(buffer ^ 1);
+      put(SETS == 2 ? BUFFER ^ 1 : 0, BUFFER ^ 1);
       lds_barrier();
+    };
+    for (int u = from; u < upto; u += 2) {
+      step(u, std::integral_constant<int, 0>());
+      if (u + 1 >= upto) break;
+      step(u + 1, std::integral_constant<int, 1>());
     }
 
 #pragma unroll
@@ -388,11 +445,17 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
 
 template <int DP, int RB>
 void launch(const TreeArgs& a, unsigned grid, bool nt, hipStream_t s) {
-  auto of = [&](auto full, auto past) { hipLaunchKernelGGL((shared_kernel<DP, RB, decltype(full)::value, decltype(past)::value>), dim3(grid), dim3(64 * WAVES), 0, s, a); };
+  auto of = [&](auto full, auto past, auto plain) {
+    hipLaunchKernelGGL((shared_kernel<DP, RB, decltype(full)::value, decltype(past)::value, decltype(plain)::value>), dim3(grid), dim3(64 * WAVES), 0, s, a);
+  };
   const std::true_type yes;
   const std::false_type no;
-  if (a.D == DP) nt ? of(yes, yes) : of(yes, no);
-  else nt ? of(no, yes) : of(no, no);
+  auto with = [&](auto plain) {
+    if (a.D == DP) nt ? of(yes, yes, plain) : of(yes, no, plain);
+    else nt ? of(no, yes, plain) : of(no, no, plain);
+  };
+  if (a.cap == 0.f && !a.slopes) with(yes);
+  else with(no);
 }
 
 }  // namespace

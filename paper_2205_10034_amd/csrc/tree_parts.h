@@ -30,14 +30,13 @@ struct TreeArgs {
   int64_t n_pages, page_stride, token_stride, head_stride, q_token, q_head, o_token, o_head;  // bytes
   PageDivisor page, kv_heads, group;  // places of a page, kv heads, query heads of a kv head
   double inverse_parts;
-  int32_t page_size, table_width, capacity, n_seqs, hq, hkv, G, T, max_new, D, window, sinks, rows, items, row_tiles, parts, may_split;
+  int32_t page_size, table_width, capacity, n_seqs, hq, hkv, G, T, max_new, D, window, sinks, rows, items, row_tiles, parts, may_split, small;  // small: sequences up to this length are not split where there is a workgroup for each
   float scale, cap, inv_cap;
 };
 
 namespace {
 
 constexpr int WAVES = 4;
-constexpr int SMALL_PLACES = 1024;   // sequences up to this length are not split where there is a workgroup for each
 // How far a score may pass the running maximum before the maximum moves (a little less than 8 log 2); weights are scaled down by 2^8.
 constexpr int LAG_BITS = 8;
 constexpr float LAG = 5.5f;
@@ -90,7 +89,7 @@ __device__ __forceinline__ Deal deal(const TreeArgs& a, int rt, int w) {
     total += mine;
     longest = tiles > longest ? tiles : longest;
   }
-  if (a.n_seqs <= a.parts && !__any(longest > SMALL_PLACES / TILE)) {
+  if (a.n_seqs <= a.parts && !__any(longest > a.small / TILE)) {
     p.one_each = true;
     p.share = 1;
     p.total = a.n_seqs;
@@ -152,9 +151,9 @@ __device__ __forceinline__ void store_row(const TreeArgs& a, int t, int h, int d
 // Calls of bfloat16 with more than SHARED_FROM rows of tokens and query heads to a kv head: keys and values reach the wavefronts through LDS
 // (attention_tree_shared.hip).
 constexpr int SHARED_FROM = 32;
-constexpr int shared_tile(int dims) { return dims <= 128 ? 64 : 32; }  // places that a workgroup takes at a time
-constexpr int shared_least(int dims) { return 256 / shared_tile(dims); }
 constexpr int shared_blocks(int rows, int dims) { return rows > 64 && dims <= 128 ? 2 : 1; }  // 16 rows each of a wavefront
+constexpr int shared_tile(int dims, int blocks) { return dims * blocks <= 64 ? 64 : 32; }    // places that a workgroup takes at a time
+constexpr int shared_least(int dims, int blocks) { return 256 / shared_tile(dims, blocks); }  // tiles of a part, at least
 int32_t launch_tree_shared(const TreeArgs& a, int blocks, unsigned grid, bool nt, hipStream_t s);
 
 }  // namespace moesys
