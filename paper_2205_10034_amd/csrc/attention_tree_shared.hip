@@ -266,8 +266,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
         for (int st = 0; st < SUB; ++st)
 #pragma unroll
           for (int i = 0; i < 4; ++i) top[rb] = fmaxf(top[rb], z[rb][st][i]);
-        if (fast) top[rb] *= c2;
-        moves |= top[rb] > m[rb] + (fast ? LAG2 : LAG);
+        // (a first score is always one, also where its power is beyond float32)
+        moves |= (fast ? top[rb] * c2 : top[rb]) > m[rb] + (fast ? LAG2 : LAG) || (m[rb] == -INFINITY && top[rb] > -INFINITY);
       }
       if (__builtin_expect(__any(moves), 0)) {
         bool far = false;
@@ -275,7 +275,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
         for (int rb = 0; rb < RB; ++rb) {
           top[rb] = fmaxf(top[rb], __shfl_xor(top[rb], 16, 64));
           top[rb] = fmaxf(top[rb], __shfl_xor(top[rb], 32, 64));
-          far |= fabsf(top[rb]) > 0x1p100f && top[rb] != -INFINITY;
+          far |= fabsf(top[rb] * c2) > 0x1p100f && top[rb] != -INFINITY;
         }
         if (__builtin_expect(fast && __any(far), 0)) {  // (as far from 0 as that, what the conversion rounds is either the same or gone)
           fast = false;
@@ -295,7 +295,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
         }
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
-          const float now = fmaxf(m[rb], top[rb]), less = m[rb] - now, f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(fast ? less : less * LOG2E);
+          const float now = fmaxf(m[rb], fast ? top[rb] * c2 : top[rb]), less = m[rb] - now, f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(fast ? less : less * LOG2E);
           m[rb] = now;
           l[rb] *= f;
 #pragma unroll
