@@ -2,10 +2,11 @@
 //   m' = max(m, z_j);  l' = l exp(m - m') + exp(z_j - m');  o' = o exp(m - m') + exp(z_j - m') v_j;  out = o / l,
 // in one pass over the places that some token of the sequence sees, split over the length into pieces that are joined at the end.
 //
-// The rows of a kv head are its new tokens times the G query heads that share it, 16 to a block of the matrix instructions, RB blocks to a
-// workgroup, so that keys and values are read once for up to 64 rows.  Bound: HBM up to about that many rows (a tile of 32 places by
-// 64 rows takes a wavefront some 1500 clocks of matrix instructions and as many of exponentials, its keys and values 6000 clocks of the
-// CU's share of the memory), the matrix and exponential units beyond, where several workgroups read the same keys through the caches.
+// The rows of a kv head are its new tokens times the G query heads that share it, 16 to a block of the matrix instructions, one or two
+// blocks to a workgroup, so that keys and values are read once for up to 32 rows; bfloat16 calls with more take attention_tree_shared.hip
+// (32 sequences of 3000 to 5000 places, 4 kv heads of 128: 32 rows 75 us here and 71 there, of 64 41 and 46, of 256 107 and 127; 64 rows
+// 104 here, with four blocks, and 80 there).  Bound: HBM, and for short or windowed calls the trips to memory at the start of a piece
+// (length, table entry, keys) and of every tile.  A tile in each wavefront's registers, the next one's loads behind the products that use it:
 //  - Scores: S^T[place, row] = K Q^T, keys as the first operand, from memory into the registers that the instruction reads.  A load
 //    brings eight keys' whole 128-byte lines; the operand wants half lines of sixteen, which is an exchange of lanes 8 apart.
 //  - Output: O^T[dim, row] += V^T P^T.  A lane of S^T holds four places of one row, which is how the second operand wants P^T when the
@@ -153,7 +154,7 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X), RB))
     // Nothing in the loop that loads is conditional: what a tile beyond the last one would load is ZEROS.  (Behind a branch the
     // compiler waits for every load in flight before it uses the first.)
     auto entry_of = [&](int u) {  // the table's entry for this lane's place of the u-th tile; an entry of the table in any case
-      const unsigned column = (unsigned)a.page.quotient((int)((unsigned)span.tile(u) * TILE + tp)), last = (unsigned)a.table_width - 1u;
+      const unsigned column = (unsigned)a.page.quotient((int)((unsigned)span.tile(u) * TILE + tp)), last = (unsigned)a.last_column;
       return table[column < last ? column : last];
     };
     // rows of the u-th tile into LDS; returns which places are there
@@ -638,7 +639,8 @@ extern "C" int32_t moe_attention_tree(const moe_kv_cache* c, int32_t n_q_heads, 
   a.q = (const char*)q->data;
   a.out = (char*)out->data;
   a.lse = lse;
-  a.table = c->page_table;
+  a.table = c->table_width > 0 ? c->page_table : (const int32_t*)ws;
+  a.last_column = c->table_width > 0 ? c->table_width - 1 : 0;
   a.lens = seq_lens;
   a.first = token_first;
   a.words = visible;

@@ -1,9 +1,12 @@
 // Attention of drafted tokens, many rows to a kv head (see attention_tree.hip): every wavefront of a workgroup has rows of its own and reads
 // the same tile of keys and values from LDS.
 //
-// With 64 rows the call is still bound by the memory: the tiles' loads must never pause.  They go through registers, a tile ahead, into the
-// other one of two tiles in LDS, so that two workgroups of a CU have 32 KB each on their way (their own tiles in every wavefront's
-// registers, as with few rows, leave room for one wavefront per SIMD and 3.5 TB/s).  From 128 rows on the matrix instructions bind.
+// Up to 64 rows the memory binds: tiles of 16 KB go through registers, up to two ahead, into the other one of two tiles in LDS, two workgroups
+// to a CU.  64 sequences of up to 8192 places, 16 tokens, 32 heads on 8 of 128: 190 us in this kernel, 5.2 TB/s; 40 of them are the
+// starts and ends of pieces, the tiles themselves come at 6.5 TB/s.  (A tile in every wavefront's own registers, one wavefront per SIMD: 280.)
+// From 128 rows on, 32 to a wavefront, a tile takes it 2000 clocks of which 770 are matrix instructions and about as many exponentials,
+// packing and addresses; two wavefronts per SIMD overlap some of that: 64 tokens on 131071 places, 270 us, 510 TFLOP/s (770 with the
+// weights' second halves).  Registers decide: 60 spilled ones cost a third of the time, since their way back waits for the tiles.
 //  - A tile's rows lie in LDS as in memory, their 16-byte chunks exchanged by key(row), so that neither the keys (16 rows, one chunk
 //    each) nor the values (8 rows, two neighbouring chunks) nor the stores meet in a bank.
 //  - Scores: S^T[place, row] = K Q^T, the queries in registers.  Output: O^T[dim, row] += V^T P^T, the values read by the transposing
@@ -92,7 +95,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
 
     // The place of lane % MINE of this wavefront's rows of the u-th tile: its table entry, and where its row lies (-1: it is not there).
     auto entry_of = [&](int u) {
-      const unsigned column = (unsigned)a.page.quotient((int)((unsigned)span.tile(u) * TILE + wave * MINE + (lane & (MINE - 1)))), last = (unsigned)a.table_width - 1u;
+      const unsigned column = (unsigned)a.page.quotient((int)((unsigned)span.tile(u) * TILE + wave * MINE + (lane & (MINE - 1)))), last = (unsigned)a.last_column;
       return table[column < last ? column : last];
     };
     auto row_of = [&](int u, int entry) {

@@ -30,6 +30,7 @@ struct TreeArgs {
   int64_t n_pages, page_stride, token_stride, head_stride, q_token, q_head, o_token, o_head;  // bytes
   PageDivisor page, kv_heads, group;  // places of a page, kv heads, query heads of a kv head
   double inverse_parts;
+  int32_t last_column;  // of the table; 0 also of one without columns, where `table` is some other memory whose entries nobody uses
   int32_t page_size, table_width, capacity, n_seqs, hq, hkv, G, T, max_new, D, window, sinks, rows, items, row_tiles, parts, may_split, small;  // small: sequences up to this length are not split where there is a workgroup for each
   float scale, cap, inv_cap;
 };

@@ -84,7 +84,7 @@ def test_scores_whose_powers_are_beyond_float32(D, G):
             p.k[at(s, j)] = 0.0
     best = {0: [7, 90, 150], 1: [3, 511, 900]}
     top = torch.tensor(big).bfloat16().float().item()
-    assert D * top * top < np.finfo(np.float32).max < D * top * top * 1.4427
+    assert D * top * top < float(np.finfo(np.float32).max) < D * top * top * 1.4427
     for s, js in best.items():
         for j in js:
             p.k[at(s, j)] = top
@@ -172,3 +172,24 @@ def test_places_beyond_32_bits():
     q, words = queries(20, 2 * hkv, D, "bf16"), tree_words([20])
     out, lse = attend_tree(cache, q, [0, 20], [200], 20, words)
     check_tree(p, q, [0, 20], [200], 20, out, lse, words)
+
+
+@pytest.mark.parametrize("width,n_pages", [(0, 0), (0, 3), (2, 0)])
+@pytest.mark.parametrize("n", [4, 20])
+def test_caches_without_columns_or_pages(n, width, n_pages):
+    """Nothing is there: outputs are zero, pages are not to be had, and nothing is read."""
+    S, hkv, hq, D = 3, 2, 8, 64
+    k = torch.zeros(n_pages, 16, hkv, D, dtype=torch.bfloat16, device="cuda")
+    cache = M.KVCache(k, torch.zeros_like(k), torch.full((S, width), -1, dtype=torch.int32, device="cuda"))
+    q = queries(S * n, hq, D, "bf16")
+    out, lse = attend_tree(cache, q, firsts([n] * S), [50, 0, 7], n)
+    assert not out.any() and np.isneginf(lse).all()
+    refs, lens = torch.zeros(n_pages, dtype=torch.int32, device="cuda"), torch.tensor([40, 16, -1], dtype=torch.int32, device="cuda")
+    ws, missing = torch.empty(M.moe_kv_pages_workspace_bytes(cache), dtype=torch.uint8, device="cuda"), torch.full((1,), -3, dtype=torch.int32, device="cuda")
+    M.moe_kv_reserve(cache, refs, lens, ws, missing=missing)
+    assert missing.item() == (3 if width else 0) and (cache.page_table == -1).all()
+    one = lambda x: torch.tensor([x], dtype=torch.int32, device="cuda")  # noqa: E731
+    M.moe_kv_fork(cache, refs, one(0), one(2), lens, ws, missing=missing)
+    M.moe_kv_release(cache, refs, lens)
+    M.moe_kv_compact(cache, lens, torch.zeros(S, 2, dtype=torch.int32, device="cuda"))
+    assert lens.tolist() == [40, 16, 40] and missing.item() == 0 and not refs.any()
