@@ -8,6 +8,7 @@
 #include "wave_util.h"
 #include <float.h>
 #include <math.h>
+#include <type_traits>
 
 namespace moesys {
 namespace {
@@ -18,7 +19,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr int THREADS = 256, WAVES = THREADS / 64;
 constexpr int PER_LANE = 16, CHUNK = 64 * PER_LANE;  // logits that a lane, a wavefront takes at a time
 constexpr int LIST = 128;                            // candidates that a wavefront holds
-constexpr int SHARED_LIST = 256;                     // ... that all of a row's do, and groups with candidates
+constexpr int FOUND = 512;                           // groups with candidates that a row's workgroup holds
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float LAG_BITS = 8.f;
 constexpr float FAR = 1024.f;  // 2^-14 of p is what lse's rounding is there
@@ -196,14 +197,17 @@ struct TopList {
   }
 };
 
-// A value that K of the lanes' (0: no value) reach: their K-th largest, cut down to the upper BITS bits.
-template <int BITS>
-__device__ __forceinline__ uint32_t reached_by(uint32_t u, int K) {
+// A value that K of the lanes' (N each, 0: no value) reach: the K-th largest, cut down to the upper BITS bits; 0 where there are fewer.
+template <int BITS, int N>
+__device__ __forceinline__ uint32_t reached_by(const uint32_t (&u)[N], int K) {
   uint32_t t = 0;
 #pragma unroll
   for (int bit = 31; bit >= 32 - BITS; --bit) {
     const uint32_t more = t | 1u << bit;
-    t = __popcll(__ballot(u >= more)) >= K ? more : t;
+    int n = 0;
+#pragma unroll
+    for (int e = 0; e < N; ++e) n += __popcll(__ballot(u[e] >= more));
+    t = n >= K ? more : t;
   }
   return t;
 }
@@ -448,16 +452,17 @@ __global__ __launch_bounds__(64) void join_kernel(RowArgs a) {
   if (threadIdx.x == 0) store_row<ENTROPY>(a, t, st, Row(st, a.scale), (float)id_logit, id);
 }
 
-// Ends the rows whose K largest logits are wanted, a workgroup of TEAM wavefronts to a row.  A bound that K of the threads' largest groups
-// reach leaves little more than K groups; their logits above it, in LDS, are ranked by counting, a key to a thread.
+// Ends the rows whose K largest logits are wanted, a workgroup of TEAM wavefronts to a row.  A bound that K of the groups' maxima reach (TEAM 1, rows of
+// up to SHORT chunks), or K of the threads' largest, leaves little more than K groups; of their logits, in LDS, those that the K-th largest leaves are
+// ranked by counting, a key to a thread.
+constexpr int SHORT = 8;
 template <typename X, int TEAM, bool ENTROPY>
 __global__ __launch_bounds__(64 * TEAM) void select_kernel(RowArgs a) {
   using G = Group<X>;
-  constexpr int N = 64 * TEAM, PER = 16 / (int)sizeof(typename G::type);
-  __shared__ __attribute__((aligned(16))) uint64_t keys[SHARED_LIST];
-  __shared__ uint32_t found[SHARED_LIST];
-  __shared__ uint32_t bounds[TEAM][2];
-  __shared__ int n_found, n_keys;
+  constexpr int N = 64 * TEAM, PER = 16 / (int)sizeof(typename G::type), KEYS = TEAM == 1 ? 512 : 1024;
+  __shared__ __attribute__((aligned(16))) uint64_t keys[KEYS];
+  __shared__ uint32_t found[FOUND], bounds[TEAM][2];
+  __shared__ int n_found, n_keys, n_left;
   const int t = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const X* x = reinterpret_cast<const X*>(a.x + (int64_t)t * a.row_stride);
   const int back = elements_behind(x, 16);
@@ -468,31 +473,53 @@ __global__ __launch_bounds__(64 * TEAM) void select_kernel(RowArgs a) {
     id = a.ids[t];
     id_logit = x[(unsigned)id < (unsigned)a.V ? id : 0];
   }
-  if (threadIdx.x == 0) n_found = n_keys = 0;
+  if (threadIdx.x == 0) n_found = n_keys = n_left = 0;
   const f32x4 mine = first_part(a, t);
-  // Groups: 16 bytes of them to a thread (chunks have 64), or, of short rows, single ones, so that most threads have some.
-  const int n_groups = row.chunks * 64;
-  const bool single = row.chunks <= 8 * TEAM;
-  uint32_t best = 0;
-  if (single) {
-#pragma unroll 4
-    for (int i = threadIdx.x; i < n_groups; i += N) {
-      const uint32_t order = G::order(row.groups[i]);
-      best = order > best ? order : best;
-    }
-  } else {
-#pragma unroll 2
-    for (int i = threadIdx.x * PER; i < n_groups; i += N * PER) {
-      const u32x4 v = *reinterpret_cast<const u32x4*>(row.groups + i);
-#pragma unroll
-      for (int e = 0; e < PER; ++e) best = G::order(v, e) > best ? G::order(v, e) : best;
-    }
-  }
   // (-infinity and NaN bound nothing)
-  if (best <= order_of(-INFINITY)) best = 0;
-  uint32_t first = reached_by<G::BITS>(best, a.K), second = first;
-  if (TEAM > 1) {
-    second = reached_by<G::BITS>(best, (a.K - 1) / TEAM + 1);
+  auto bounding = [](uint32_t order) { return order <= order_of(-INFINITY) ? 0u : order; };
+  auto find = [&](uint32_t order, int group, uint32_t bound) {
+    if (order < bound) return;
+    const int at = atomicAdd(&n_found, 1);
+    if (at < FOUND) found[at] = group;
+  };
+  const int n_groups = row.chunks * 64;
+  uint32_t bound;
+  if constexpr (TEAM == 1) {
+    uint32_t order[SHORT], u[SHORT];
+#pragma unroll
+    for (int c = 0; c < SHORT; ++c) order[c] = c < row.chunks ? G::order(row.groups[c * 64 + lane]) : 0;
+#pragma unroll
+    for (int c = 0; c < SHORT; ++c) u[c] = bounding(order[c]);
+    bound = reached_by<G::BITS>(u, a.K);
+    int n = 0;
+#pragma unroll
+    for (int c = 0; c < SHORT; ++c) {
+      if (c >= row.chunks) break;
+      const unsigned long long all = __ballot(order[c] >= bound);
+      if (order[c] >= bound) found[n + __popcll(all & ((1ull << lane) - 1))] = c * 64 + lane;
+      n += __popcll(all);
+    }
+    if (lane == 0) n_found = n;
+  } else {
+    // 16 bytes of groups to a thread (chunks have 64), or, of shorter rows, single ones, so that every thread has some
+    const bool single = row.chunks <= 8 * TEAM;
+    uint32_t best[1] = {0};
+    if (single) {
+#pragma unroll 4
+      for (int i = threadIdx.x; i < n_groups; i += N) {
+        const uint32_t order = G::order(row.groups[i]);
+        best[0] = order > best[0] ? order : best[0];
+      }
+    } else {
+#pragma unroll 2
+      for (int i = threadIdx.x * PER; i < n_groups; i += N * PER) {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(row.groups + i);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) best[0] = G::order(v, e) > best[0] ? G::order(v, e) : best[0];
+      }
+    }
+    best[0] = bounding(best[0]);
+    uint32_t first = reached_by<G::BITS>(best, a.K), second = reached_by<G::BITS>(best, (a.K - 1) / TEAM + 1);
     if (lane == 0) {
       bounds[wave][0] = first;
       bounds[wave][1] = second;
@@ -503,26 +530,18 @@ __global__ __launch_bounds__(64 * TEAM) void select_kernel(RowArgs a) {
       first = bounds[w][0] > first ? bounds[w][0] : first;
       second = bounds[w][1] < second ? bounds[w][1] : second;
     }
-  }
-  // At least K logits reach the larger of these: K threads of one wavefront do, or a TEAM-th of K in each.
-  const uint32_t bound = first > second ? first : second;
-  if (single) {
+    // At least K logits reach the larger of these: K threads of one wavefront do, or a TEAM-th of K in each.
+    bound = first > second ? first : second;
+    if (single) {
 #pragma unroll 4
-    for (int i = threadIdx.x; i < n_groups; i += N)
-      if (G::order(row.groups[i]) >= bound) {
-        const int at = atomicAdd(&n_found, 1);
-        if (at < SHARED_LIST) found[at] = i;
-      }
-  } else {
+      for (int i = threadIdx.x; i < n_groups; i += N) find(G::order(row.groups[i]), i, bound);
+    } else {
 #pragma unroll 2
-    for (int i = threadIdx.x * PER; i < n_groups; i += N * PER) {
-      const u32x4 v = *reinterpret_cast<const u32x4*>(row.groups + i);
+      for (int i = threadIdx.x * PER; i < n_groups; i += N * PER) {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(row.groups + i);
 #pragma unroll
-      for (int e = 0; e < PER; ++e)
-        if (G::order(v, e) >= bound) {
-          const int at = atomicAdd(&n_found, 1);
-          if (at < SHARED_LIST) found[at] = i + e;
-        }
+        for (int e = 0; e < PER; ++e) find(G::order(v, e), i + e, bound);
+      }
     }
   }
   const Stats st = join_parts<ENTROPY>(a, t, mine);
@@ -534,7 +553,7 @@ __global__ __launch_bounds__(64 * TEAM) void select_kernel(RowArgs a) {
   };
   lds_barrier();
   const int groups = n_found;
-  if (groups <= SHARED_LIST) {
+  if (groups <= FOUND) {
     for (int i0 = wave * 64; i0 < groups; i0 += N) {
       const bool have = i0 + lane < groups;
       const uint32_t at = have ? found[i0 + lane] : 0;
@@ -554,7 +573,7 @@ __global__ __launch_bounds__(64 * TEAM) void select_kernel(RowArgs a) {
       places(have ? __popc(mask) : 0, place, all);
       int begin = lane == 0 ? atomicAdd(&n_keys, all) : 0;
       place += __builtin_amdgcn_readfirstlane(begin);
-      if (!have || place + __popc(mask) > SHARED_LIST) mask = 0;
+      if (!have || place + __popc(mask) > KEYS) mask = 0;
 #pragma unroll
       for (int l = 0; l < loads<X>; ++l)
 #pragma unroll
@@ -562,8 +581,36 @@ __global__ __launch_bounds__(64 * TEAM) void select_kernel(RowArgs a) {
           if (mask >> (l * per_load<X> + e) & 1) keys[place++] = key_of(order_of(element((const X*)nullptr, v[l], e)), (int)(j0 + l * 64 * per_load<X> + e));
     }
     lds_barrier();
-    const int n = n_keys;
-    if (n <= SHARED_LIST) {
+    int n = n_keys;
+    if (n <= KEYS) {
+      // Only those that the K-th largest leaves: 16 or 32 steps over what a lane has of them, where counting takes a step for each of them all.
+      auto leave = [&](auto slots) {
+        constexpr int SLOTS = decltype(slots)::value, OWN = (SLOTS + TEAM - 1) / TEAM;
+        uint32_t order[SLOTS];
+#pragma unroll
+        for (int e = 0; e < SLOTS; ++e) order[e] = e * 64 + lane < n ? (uint32_t)(keys[e * 64 + lane] >> 32) : 0;
+        const uint32_t least = reached_by<8 * (int)sizeof(X)>(order, a.K);
+        uint64_t own[OWN];
+#pragma unroll
+        for (int e = 0; e < OWN; ++e) own[e] = e * N + (int)threadIdx.x < n ? keys[e * N + threadIdx.x] : 0;
+        lds_barrier();
+#pragma unroll
+        for (int e = 0; e < OWN; ++e) {
+          const bool stays = e * N + (int)threadIdx.x < n && (uint32_t)(own[e] >> 32) >= least;
+          const unsigned long long all = __ballot(stays);
+          if (!all) continue;
+          int begin = lane == 0 ? atomicAdd(&n_left, __popcll(all)) : 0;
+          begin = __builtin_amdgcn_readfirstlane(begin);
+          if (stays) keys[begin + __popcll(all & ((1ull << lane) - 1))] = own[e];
+        }
+        lds_barrier();
+        n = n_left;
+      };
+      if (n > 64 && n > a.K + a.K / 4) {
+        if (n <= 128) leave(std::integral_constant<int, 2>());
+        else if (n <= 256) leave(std::integral_constant<int, 4>());
+        else leave(std::integral_constant<int, KEYS / 64>());
+      }
       for (int i = n + threadIdx.x; i < ((n + 7) & ~7); i += N) keys[i] = 0;  // (above none)
       lds_barrier();
       for (int i0 = wave * 64; i0 < n; i0 += N) {
@@ -606,9 +653,6 @@ Division division_of(int T, int V, int K) {
   return d;
 }
 
-// Whether one wavefront finds a row's largest: of short rows, with several lanes to each of the K, or the bound is too low.
-bool select_alone(int chunks, int K) { return chunks <= 2 || (chunks <= 8 && K <= 16); }
-
 template <typename X, bool ENTROPY, bool TOP>
 int32_t launch_rows(const RowArgs& a, const Division& d, hipStream_t s) {
   const int64_t units = (int64_t)a.T * d.parts;
@@ -617,7 +661,7 @@ int32_t launch_rows(const RowArgs& a, const Division& d, hipStream_t s) {
   int32_t st = check_hip(hipGetLastError(), "log-probabilities launch");
   if (st != MOE_OK || (d.parts == 1 && !TOP)) return st;
   if constexpr (TOP) {
-    if (select_alone(d.max_chunks, a.K)) hipLaunchKernelGGL((select_kernel<X, 1, ENTROPY>), dim3((unsigned)a.T), dim3(64), 0, s, a);
+    if (d.max_chunks <= SHORT) hipLaunchKernelGGL((select_kernel<X, 1, ENTROPY>), dim3((unsigned)a.T), dim3(64), 0, s, a);
     else hipLaunchKernelGGL((select_kernel<X, WAVES, ENTROPY>), dim3((unsigned)a.T), dim3(64 * WAVES), 0, s, a);
   } else {
     hipLaunchKernelGGL((join_kernel<X, ENTROPY>), dim3((unsigned)a.T), dim3(64), 0, s, a);

@@ -73,6 +73,18 @@ def test_sizes(T, V, K, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,V,K", [(40, 120, 20), (40, 120, 64), (33, 300, 20), (20, 500, 64), (20, 700, 63), (20, 1024, 64), (15, 1900, 64), (15, 2500, 64), (9, 8000, 64), (9, 8192, 17), (5, 9000, 64),
+                                   (5, 33000, 64), (3, 70000, 33)])
+def test_alternatives_of_rows_of_every_length(T, V, K, dtype):
+    """One wavefront or four to a row, as many groups as alternatives and fewer, more candidates than are ranked at once."""
+    for seed in range(3):
+        x, h = logits(T, V, dtype, seed=seed)
+        check(forward(x, [0] * T, K), h, [0] * T, K)
+    x.copy_(torch.from_numpy(np.round(h)).to(DT[dtype]))          # many ties
+    check(forward(x, [0] * T, K), x.float().cpu().numpy(), [0] * T, K)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("offset", [0, 1, 3, 4, 7])
 def test_alignments(offset, dtype):
     for V, stride in ((1, 1), (5, 9), (131, 131), (1027, 1032), (9001, 9003), (70001, 70007)):
