@@ -476,13 +476,13 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X), RB))
   }
 }
 
-// Joins the pieces of (token, query head) rows in their order, a wavefront to a row; sequences of one piece are complete already.
+// Joins the pieces of (token, query head) rows in their order, LANES lanes to a row (four dims each); sequences of one piece are complete already.
 constexpr int JOIN_THREADS = 256;
-template <typename X>
+template <typename X, int LANES>
 __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(TreeArgs a) {
   constexpr int AHEAD = 8;
-  const int64_t id = (int64_t)blockIdx.x * (JOIN_THREADS / 64) + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63, s = (int)(id / (a.max_new * a.hq)), rest = (int)(id - (int64_t)s * a.max_new * a.hq), i = rest / a.hq, h = rest - i * a.hq;
+  const int64_t id = (int64_t)blockIdx.x * (JOIN_THREADS / LANES) + threadIdx.x / LANES;
+  const int lane = threadIdx.x % LANES, s = (int)(id / (a.max_new * a.hq)), rest = (int)(id - (int64_t)s * a.max_new * a.hq), i = rest / a.hq, h = rest - i * a.hq;
   if (s >= a.n_seqs) return;
   const Drafts d = drafts(a, s);
   if (i >= d.n) return;
@@ -491,19 +491,19 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(TreeArgs a) {
   if (plan.y <= 1) return;
   auto row = [&](int j) { return ((int64_t)piece_slot(plan.x, j) * a.items + item) * a.rows + r; };
   float top = -INFINITY, sum = 0.f;
-  for (int j = lane; j < plan.y; j += 64) top = fmaxf(top, a.part_ml[row(j)][0]);
+  for (int j = lane; j < plan.y; j += LANES) top = fmaxf(top, a.part_ml[row(j)][0]);
 #pragma unroll
-  for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
+  for (int x = LANES / 2; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
   const int dim = lane * 4;
   f32x4 y{0.f, 0.f, 0.f, 0.f};
-  for (int j0 = 0; j0 < plan.y; j0 += 64) {
+  for (int j0 = 0; j0 < plan.y; j0 += LANES) {
     float f = 0.f;
     if (j0 + lane < plan.y) {
       const f32x2 ml = a.part_ml[row(j0 + lane)];
       f = top == -INFINITY ? 1.f : power(ml[0] - top);
       sum += f * ml[1];
     }
-    const int n = plan.y - j0 < 64 ? plan.y - j0 : 64;
+    const int n = plan.y - j0 < LANES ? plan.y - j0 : LANES;
     for (int j = 0; j < n; j += AHEAD) {
       f32x4 part[AHEAD];
 #pragma unroll
@@ -511,11 +511,11 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(TreeArgs a) {
         part[e] = j + e < n && dim < a.D ? *reinterpret_cast<const f32x4*>(a.part_o + row(j0 + j + e) * a.D + dim) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int e = 0; e < AHEAD; ++e)
-        if (j + e < n) y += __shfl(f, j + e, 64) * part[e];
+        if (j + e < n) y += __shfl(f, j + e, LANES) * part[e];
     }
   }
 #pragma unroll
-  for (int x = 32; x; x >>= 1) sum += __shfl_xor(sum, x, 64);
+  for (int x = LANES / 2; x; x >>= 1) sum += __shfl_xor(sum, x, 64);
   if (dim < a.D) store_row<X>(a, d.first + i, h, dim, y, sum, top);
 }
 
@@ -585,7 +585,13 @@ int32_t launch_tree(const TreeArgs& a, const Split& sp, hipStream_t s) {
   const int32_t st = check_hip(hipGetLastError(), "tree attention launch");
   if (st != MOE_OK || !sp.may_split) return st;
   const int64_t rows = (int64_t)a.n_seqs * a.max_new * a.hq;
-  hipLaunchKernelGGL(join_kernel<X>, dim3((unsigned)((rows + JOIN_THREADS / 64 - 1) / (JOIN_THREADS / 64))), dim3(JOIN_THREADS), 0, s, a);
+  auto join = [&](auto lanes) {
+    constexpr int LANES = decltype(lanes)::value, PER = JOIN_THREADS / LANES;
+    hipLaunchKernelGGL((join_kernel<X, LANES>), dim3((unsigned)((rows + PER - 1) / PER)), dim3(JOIN_THREADS), 0, s, a);
+  };
+  if (a.D <= 64) join(std::integral_constant<int, 16>());
+  else if (a.D <= 128) join(std::integral_constant<int, 32>());
+  else join(std::integral_constant<int, 64>());
   return check_hip(hipGetLastError(), "tree attention join launch");
 }
 
