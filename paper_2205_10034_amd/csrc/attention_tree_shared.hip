@@ -193,8 +193,27 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
       for (int st = 0; st < SUB; ++st) key[ks & 1][st] = *reinterpret_cast<const bf16x8*>(tiles[buffer][0] + ((key_at ^ ks << 6) + st * 16 * PITCH));
     };
     auto read_values = [&](int buffer, int n) { return values_of(tiles[buffer][1] + ((value_at ^ (n % NDB) << 5) + n / NDB * 32 * PITCH), 16 * PITCH); };
-    auto compute = [&](int u, int buffer, uint64_t here, bf16x8 (&key)[2][SUB]) {
-      const int p0 = span.tile(u) * TILE;
+    // Which places of a tile this lane's rows see, 4 SUB bits to a row.
+    auto seen_of = [&](int p0, uint64_t here, uint32_t (&bits)[RB]) {
+      uint64_t seen[RB];
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        seen[rb] = seen_lds[(wave * RB + rb) * 16 + m16];
+        bits[rb] = 0;
+      }
+#pragma unroll
+      for (int st = 0; st < SUB; ++st)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int p = p0 + st * 16 + g * 4 + i, j = p - d.base, jj = j & (MOE_MAX_DRAFTS - 1);  // (places that are there have j < n)
+          const uint32_t is_there = (uint32_t)(here >> (st * 16 + g * 4 + i)) & 1, cached = j < 0;
+          const int pos_p = cached ? p : d.base + depth_lds[jj];
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb)
+            bits[rb] |= (is_there & (cached | (uint32_t)(seen[rb] >> jj)) & (uint32_t)in_window(pos[rb], pos_p, p, a.window, a.sinks)) << (st * 4 + i);
+        }
+    };
+    auto compute = [&](int p0, int buffer, uint64_t here, bool masked, bf16x8 (&key)[2][SUB]) {
       f32x4 z[RB][SUB];
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb)
@@ -209,7 +228,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
         if (ks + 2 < KSTEPS) read_keys(key, buffer, ks + 2);
         __builtin_amdgcn_sched_barrier(0);
       }
-      const bool with_drafts = p0 + TILE > d.base;
       if constexpr (!PLAIN) {
 #pragma unroll
         for (int st = 0; st < SUB; ++st)
@@ -217,7 +235,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
           for (int i = 0; i < 4; ++i) {
             const int p = p0 + st * 16 + g * 4 + i;
             int pos_p = p;
-            if (with_drafts && p >= d.base) pos_p = d.base + depth_lds[p - d.base < MOE_MAX_DRAFTS ? p - d.base : 0];
+            if (p0 + TILE > d.base && p >= d.base) pos_p = d.base + depth_lds[p - d.base < MOE_MAX_DRAFTS ? p - d.base : 0];
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
               float s = z[rb][st][i] * a.scale;
@@ -231,31 +249,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
 #pragma unroll
           for (int st = 0; st < SUB; ++st) z[rb][st] *= a.scale;
       }
-      // Everyone sees everything of a tile that is all there, before the new tokens, and in the window of the last position or among
-      // the sinks.
-      const bool masked = here != EVERY || with_drafts || (a.window > 0 && last_pos - p0 >= a.window && p0 + TILE > a.sinks);
-      uint32_t seen_here[RB] = {};  // places that this lane's rows see, 4 SUB bits
       if (__builtin_expect(masked, 0)) {
-        uint64_t seen[RB];
+        uint32_t bits[RB];
+        seen_of(p0, here, bits);
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-          seen[rb] = seen_lds[(wave * RB + rb) * 16 + m16];
-          seen_here[rb] = 0;
-        }
+        for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-        for (int st = 0; st < SUB; ++st)
+          for (int st = 0; st < SUB; ++st)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int p = p0 + st * 16 + g * 4 + i, j = p - d.base, jj = j & (MOE_MAX_DRAFTS - 1);  // (places that are there have j < n)
-            const uint32_t is_there = (uint32_t)(here >> (st * 16 + g * 4 + i)) & 1, cached = j < 0;
-            const int pos_p = cached ? p : d.base + depth_lds[jj];
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb) {
-              const uint32_t ok = is_there & (cached | (uint32_t)(seen[rb] >> jj)) & (uint32_t)in_window(pos[rb], pos_p, p, a.window, a.sinks);
-              z[rb][st][i] = ok ? z[rb][st][i] : -INFINITY;
-              seen_here[rb] |= ok << (st * 4 + i);
-            }
-          }
+            for (int i = 0; i < 4; ++i) z[rb][st][i] = bits[rb] >> (st * 4 + i) & 1 ? z[rb][st][i] : -INFINITY;
       }
       // The maximum moves only when some score passes it by a factor of nearly 2^8, so that the four lanes of a row need not exchange
       // theirs.  All weights are 2^-8 of what they would be (sums, and so lse, with them): none is above 1, and no product with a
@@ -305,19 +307,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
           for (int db = 0; db < NDB; ++db) o[rb][db] *= f;
         }
       }
-      // A value that is not finite and that only some rows see would reach the others as 0 times it: it is left out of the product, and
-      // its element of the rows that see it becomes NaN.
-      bool odd = false;
-      if (__builtin_expect(masked, 0)) {
-        uint32_t any = 0;
-#pragma unroll
-        for (int n = 0; n < VALUES; ++n) {
-          const u32x4 bits = __builtin_bit_cast(u32x4, read_values(buffer, n));
-#pragma unroll
-          for (int i = 0; i < 4; ++i) any |= not_finite(bits[i]);
-        }
-        odd = __any(any != 0);
-      }
       bf16x8 value[AHEAD];
 #pragma unroll
       for (int n = 0; n < AHEAD; ++n) value[n] = read_values(buffer, n);
@@ -360,31 +349,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
       // two blocks of dims at a time: four or more products between two of the same sum
 #pragma unroll
       for (int n0 = 0; n0 < VALUES; n0 += 2) {
-        if (__builtin_expect(odd, 0)) {  // (out of the way: a jump over it costs as much as two products)
-#pragma unroll
-          for (int n = n0; n < n0 + 2; ++n) {
-            u32x4 bits = __builtin_bit_cast(u32x4, value[n % AHEAD]), bad;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              bad[i] = not_finite(bits[i]);
-              bits[i] &= ~((bad[i] & 0xffffu ? 0xffffu : 0u) | (bad[i] >> 16 ? 0xffff0000u : 0u));
-            }
-            value[n % AHEAD] = __builtin_bit_cast(bf16x8, bits);
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb) {
-              u32x4 see;
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const uint32_t s = seen_here[rb] >> ((2 * (n / NDB) + i / 2) * 4 + i % 2 * 2);
-                see[i] = (s & 1 ? 0x3f80u : 0u) | (s & 2 ? 0x3f800000u : 0u);
-              }
-              const f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, bad), __builtin_bit_cast(bf16x8, see), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (hit[i] > 0.f) o[rb][n % NDB][i] = NAN;
-            }
-          }
-        }
 #pragma unroll
         for (int part = 0; part < 2; ++part)
 #pragma unroll
@@ -399,6 +363,56 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
       }
     };
 
+    // A value that is not finite and that only some rows see would reach the others as 0 times it: its element of the rows that see it becomes
+    // NaN, and it leaves the tile.  (All wavefronts find the same.  Nothing of this is in the way of other tiles: a jump over it beside every
+    // product, or a second loop of products, costs more than the products.)
+    auto without_odd_values = [&](int p0, int buffer, uint64_t here) __attribute__((always_inline)) {
+      uint32_t any = 0;
+#pragma unroll 1
+      for (int n = 0; n < VALUES; ++n) {
+        const u32x4 bits = __builtin_bit_cast(u32x4, read_values(buffer, n));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) any |= not_finite(bits[i]);
+      }
+      if (__builtin_expect(!__any(any != 0), 1)) return;
+      if (active) {
+        uint32_t seen[RB];
+        seen_of(p0, here, seen);
+#pragma unroll
+        for (int n = 0; n < VALUES; ++n) {
+          u32x4 bad = __builtin_bit_cast(u32x4, read_values(buffer, n));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) bad[i] = not_finite(bad[i]);
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb) {
+            u32x4 see;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t s = seen[rb] >> ((2 * (n / NDB) + i / 2) * 4 + i % 2 * 2);
+              see[i] = (s & 1 ? 0x3f80u : 0u) | (s & 2 ? 0x3f800000u : 0u);
+            }
+            const f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, bad), __builtin_bit_cast(bf16x8, see), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (hit[i] > 0.f) o[rb][n % NDB][i] = NAN;
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      lds_barrier();  // (all have looked)
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        u32x4* at = reinterpret_cast<u32x4*>(tiles[buffer][1] + store_at[i]);
+        u32x4 bits = *at;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t bad = not_finite(bits[e]);
+          bits[e] &= ~((bad & 0xffffu ? 0xffffu : 0u) | (bad >> 16 ? 0xffff0000u : 0u));
+        }
+        *at = bits;
+      }
+      lds_barrier();
+    };
     auto step = [&](int u, auto parity) __attribute__((always_inline)) {
       constexpr int BUFFER = decltype(parity)::value;
       bf16x8 key[2][SUB];
@@ -411,7 +425,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
       place(row_of(u + SETS + 1, entry));
       entry = entry_of(u + SETS + 2);
       __builtin_amdgcn_sched_barrier(0);  // (they are on their way while the tile is worked on)
-      if (active) compute(u, BUFFER, here, key);
+      const int p0 = span.tile(u) * TILE;
+      // Everyone sees everything of a tile that is all there, before the new tokens, and in the window of the last position or among
+      // the sinks.
+      const bool masked = here != EVERY || p0 + TILE > d.base || (a.window > 0 && last_pos - p0 >= a.window && p0 + TILE > a.sinks);
+      if (__builtin_expect(masked, 0)) without_odd_values(p0, BUFFER, here);
+      if (active) compute(p0, BUFFER, here, masked, key);
       __builtin_amdgcn_sched_barrier(0);
       put(SETS == 2 ? BUFFER ^ 1 : 0, BUFFER ^ 1);
       lds_barrier();
