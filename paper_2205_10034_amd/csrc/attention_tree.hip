@@ -270,7 +270,7 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X), RB))
         // the sinks.
         const bool masked = here != EVERY || with_drafts || (a.window > 0 && last_pos - p0 >= a.window && p0 + TILE > a.sinks);
         uint32_t seen_here = 0;  // places that this lane's rows see, 4 SUB bits to a row
-        if (masked) {
+        if (__builtin_expect(masked, 0)) {
           uint64_t seen[RB];
 #pragma unroll
           for (int rb = 0; rb < RB; ++rb) seen[rb] = seen_lds[rb * 16 + m16];
@@ -303,7 +303,7 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X), RB))
             for (int i = 0; i < 4; ++i) top[rb] = fmaxf(top[rb], z[rb][st][i]);
           moves |= top[rb] > m[rb] + LAG;
         }
-        if (__any(moves)) {
+        if (__builtin_expect(__any(moves), 0)) {
 #pragma unroll
           for (int rb = 0; rb < RB; ++rb) {
             float t = fmaxf(top[rb], __shfl_xor(top[rb], 16, 64));
@@ -327,10 +327,10 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X), RB))
               z[rb][st][i] = power(z[rb][st][i] - mref[rb]) * (1.f / (1 << LAG_BITS));
               l[rb] += z[rb][st][i];
             }
-        // A value that is not finite and that only some rows see would reach the others as 0 times it: it is left out of the
-        // product, and its element of the rows that see it becomes NaN.
+        // A value that is not finite and that only some rows see would reach the others as 0 times it: its element of the rows that see it
+        // becomes NaN, and it leaves the tile.
         bool odd = false;
-        if (masked) {
+        if (__builtin_expect(masked, 0)) {
 #pragma unroll
           for (int u = 0; u < NV; ++u)
 #pragma unroll
@@ -341,6 +341,60 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X), RB))
                 else odd |= not_finite(__uint_as_float(vr[u][blk][e])) != 0.f;
               }
           odd = __any(odd);
+        }
+        if (__builtin_expect(odd, 0)) {
+          if constexpr (BF16) {
+#pragma unroll
+            for (int blk = 0; blk < NBLK; ++blk)
+#pragma unroll
+              for (int j = 0; j < EPL; ++j) {
+                uint32_t bad[2 * SUB];
+#pragma unroll
+                for (int i = 0; i < 2 * SUB; ++i)
+                  bad[i] = not_finite(__builtin_amdgcn_perm(vr[2 * i + 1][blk][j / 2], vr[2 * i][blk][j / 2], j & 1 ? 0x07060302u : 0x05040100u));
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) {
+                  uint32_t see[2 * SUB];
+#pragma unroll
+                  for (int i = 0; i < 2 * SUB; ++i) {
+                    const uint32_t bits = seen_here >> ((rb * SUB + i / 2) * 4 + i % 2 * 2);
+                    see[i] = (bits & 1 ? 0x3f80u : 0u) | (bits & 2 ? 0x3f800000u : 0u);
+                  }
+                  const f32x4 hit = weighted<SUB>(bad, see, f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                  for (int i = 0; i < 4; ++i)
+                    if (hit[i] > 0.f) o[rb][blk][j][i] = NAN;
+                }
+                __builtin_amdgcn_sched_barrier(0);
+              }
+#pragma unroll
+            for (int u = 0; u < NV; ++u)
+#pragma unroll
+              for (int blk = 0; blk < NBLK; ++blk)
+#pragma unroll
+                for (int e = 0; e < (int)(sizeof(VWord) / 4); ++e) {
+                  const uint32_t bad = not_finite(vr[u][blk][e]);
+                  vr[u][blk][e] &= ~((bad & 0xffffu ? 0xffffu : 0u) | (bad >> 16 ? 0xffff0000u : 0u));
+                }
+          } else {
+#pragma unroll
+            for (int blk = 0; blk < NBLK; ++blk)
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < EPL; ++j) {
+                  const float bad = not_finite(__uint_as_float(vr[i][blk][j]));
+                  if (bad != 0.f) vr[i][blk][j] = 0u;
+#pragma unroll
+                  for (int rb = 0; rb < RB; ++rb) {
+                    const f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x4f32(bad, (seen_here >> (rb * SUB * 4 + i)) & 1 ? 1.f : 0.f, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                      if (hit[e] > 0.f) o[rb][blk][j][e] = NAN;
+                  }
+                  __builtin_amdgcn_sched_barrier(0);
+                }
+          }
         }
         if constexpr (BF16) {
           // A weight enters as the sum of two bfloat16 numbers, each rounded to nearest: 17 bits of it, an error that half a step of the
@@ -363,27 +417,6 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X), RB))
 #pragma unroll
               for (int i = 0; i < 2 * SUB; ++i)
                 vt[i] = __builtin_amdgcn_perm(vr[2 * i + 1][blk][j / 2], vr[2 * i][blk][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
-              if (odd) {
-                uint32_t bad[2 * SUB];
-#pragma unroll
-                for (int i = 0; i < 2 * SUB; ++i) {
-                  bad[i] = not_finite(vt[i]);
-                  vt[i] &= ~((bad[i] & 0xffffu ? 0xffffu : 0u) | (bad[i] >> 16 ? 0xffff0000u : 0u));
-                }
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb) {
-                  uint32_t see[2 * SUB];
-#pragma unroll
-                  for (int i = 0; i < 2 * SUB; ++i) {
-                    const uint32_t bits = seen_here >> ((rb * SUB + i / 2) * 4 + i % 2 * 2);
-                    see[i] = (bits & 1 ? 0x3f80u : 0u) | (bits & 2 ? 0x3f800000u : 0u);
-                  }
-                  const f32x4 hit = weighted<SUB>(bad, see, f32x4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-                  for (int i = 0; i < 4; ++i)
-                    if (hit[i] > 0.f) o[rb][blk][j][i] = NAN;
-                }
-              }
 #pragma unroll
               for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
@@ -396,18 +429,7 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X), RB))
             for (int i = 0; i < 4; ++i)
 #pragma unroll
               for (int j = 0; j < EPL; ++j) {
-                float v = __uint_as_float(vr[i][blk][j]);
-                if (odd) {
-                  const float bad = not_finite(v);
-                  if (bad != 0.f) v = 0.f;
-#pragma unroll
-                  for (int rb = 0; rb < RB; ++rb) {
-                    const f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x4f32(bad, (seen_here >> (rb * SUB * 4 + i)) & 1 ? 1.f : 0.f, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                      if (hit[e] > 0.f) o[rb][blk][j][e] = NAN;
-                  }
-                }
+                const float v = __uint_as_float(vr[i][blk][j]);
 #pragma unroll
                 for (int rb = 0; rb < RB; ++rb) o[rb][blk][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, z[rb][0][i], o[rb][blk][j], 0, 0, 0);
               }
