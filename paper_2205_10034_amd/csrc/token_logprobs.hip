@@ -22,7 +22,8 @@ constexpr int LIST = 128;                            // candidates that a wavefr
 constexpr int FOUND = 512;                           // groups with candidates that a row's workgroup holds
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float LAG_BITS = 8.f;
-constexpr float FAR = 1024.f;  // 2^-14 of p is what lse's rounding is there
+// Where lse's rounding shows in p: 2^-14 of it there in bfloat16 (a gradient is rounded to 2^-9), 2^-18 in float32.
+template <typename X> constexpr float far_lse = sizeof(X) == 2 ? 1024.f : 64.f;
 
 // 16 bytes of logits at any alignment of their elements
 template <typename X> struct __attribute__((packed, aligned(sizeof(X)))) Unaligned {
@@ -737,7 +738,7 @@ __global__ __launch_bounds__(THREADS) void gradient_kernel(GradArgs a) {
   // value that leaves nothing).  One wavefront has all of such a row then, whose sum it takes again before it writes (x may be y).
   float m = 0.f, log_s = lse;
   int from = c0, upto = c1;
-  if (fabsf(lse) > FAR) {
+  if (fabsf(lse) > far_lse<X>) {
     if (part != 0) return;
     Stats st{-INFINITY, 0.f, 0.f};
     upto = all_chunks;
