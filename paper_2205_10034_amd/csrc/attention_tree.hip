@@ -4,8 +4,8 @@
 //
 // The rows of a kv head are its new tokens times the G query heads that share it, 16 to a block of the matrix instructions, one or two
 // blocks to a workgroup, so that keys and values are read once for up to 32 rows; bfloat16 calls with more take attention_tree_shared.hip
-// (32 sequences of 3000 to 5000 places, 4 kv heads of 128: 32 rows 75 us here and 71 there, of 64 41 and 46, of 256 107 and 127; 64 rows
-// 104 here, with four blocks, and 80 there).  Bound: HBM, and for short or windowed calls the trips to memory at the start of a piece
+// (32 sequences of 3000 to 5000 places, 4 kv heads of 128: 32 rows 71 us here and as many there, of 64 40 and 46, of 256 105 and 127; 64 rows
+// 104 here, with four blocks, and 78 there).  Bound: HBM, and for short or windowed calls the trips to memory at the start of a piece
 // (length, table entry, keys) and of every tile.  A tile in each wavefront's registers, the next one's loads behind the products that use it:
 //  - Scores: S^T[place, row] = K Q^T, keys as the first operand, from memory into the registers that the instruction reads.  A load
 //    brings eight keys' whole 128-byte lines; the operand wants half lines of sixteen, which is an exchange of lanes 8 apart.

@@ -2,10 +2,10 @@
 // the same tile of keys and values from LDS.
 //
 // Up to 64 rows the memory binds: tiles of 16 KB go through registers, up to two ahead, into the other one of two tiles in LDS, two workgroups
-// to a CU.  64 sequences of up to 8192 places, 16 tokens, 32 heads on 8 of 128: 190 us in this kernel, 5.2 TB/s; 40 of them are the
+// to a CU.  64 sequences of up to 8192 places, 16 tokens, 32 heads on 8 of 128: 187 us in this kernel, 5.3 TB/s; some 30 of them are the
 // starts and ends of pieces, the tiles themselves come at 6.5 TB/s.  (A tile in every wavefront's own registers, one wavefront per SIMD: 280.)
 // From 128 rows on, 32 to a wavefront, a tile takes it 2000 clocks of which 770 are matrix instructions and about as many exponentials,
-// packing and addresses; two wavefronts per SIMD overlap some of that: 64 tokens on 131071 places, 270 us, 510 TFLOP/s (770 with the
+// packing and addresses; two wavefronts per SIMD overlap some of that: 64 tokens on 131071 places, 251 us, 550 TFLOP/s (820 with the
 // weights' second halves).  Registers decide: 60 spilled ones cost a third of the time, since their way back waits for the tiles.
 //  - A tile's rows lie in LDS as in memory, their 16-byte chunks exchanged by key(row), so that neither the keys (16 rows, one chunk
 //    each) nor the values (8 rows, two neighbouring chunks) nor the stores meet in a bank.
