@@ -639,7 +639,10 @@ struct Division {
 Division division_of(int T, int V, int K) {
   const int chunks = most_chunks(V, 16, 2);
   Division d{chunks <= 2 ? 1 : WAVES, 1, chunks, chunks, 0, 256};
-  if (chunks > 16) {
+  // Without alternatives, whose kernel joins the parts as well, a split costs a launch: rows of up to 65536 logits, and 256 of
+  // any length, are faster whole (us, split / whole: 1 row of 50001 bfloat16 logits 11.8 / 8.2, of 250000 11.0 / 19.0; 200 of 250000 22.5 / 26.9; 300 of 128000
+  // 18.1 / 16.8; 1000 float32 rows of 32003 26.8 / 24.0).
+  if (chunks > 16 && (K > 0 || (T < 256 && chunks > 64))) {
     int64_t parts = T > 0 ? 2048 / T : 1;
     const int64_t most = (chunks + 7) / 8;
     if (parts > most) parts = most;
