@@ -161,6 +161,18 @@ def test_forks_into_one_sequence_or_from_one_that_is_written(S, width):
     pool.fork([], [], lens)
 
 
+@pytest.mark.parametrize("S,width", [(9, 6), (5000, 4)])
+def test_one_sequence_forked_into_several(S, width):
+    pool = Pool(S, width, S * 2 + 40, 16, hkv=2, D=16)
+    lens = [50 if s == 0 else 7 for s in range(S)]
+    pool.reserve(lens)
+    lens = pool.fork([0, 0, 0, 1], [3, 4, S - 1, 5], lens)
+    assert lens[3] == lens[4] == lens[S - 1] == 50 and max(pool.refs.cpu().tolist()) == 4
+    lens = pool.fork([3, 4], [6, 7], lens)                                 # a copy of a copy
+    pool.reserve(lens, more=30)
+    pool.release([0 if s % 2 else n for s, n in enumerate(lens)])
+
+
 def test_entries_that_name_no_page():
     pool = Pool(4, 6, 30, 16)
     lens = [90, 50, 70, 0]
