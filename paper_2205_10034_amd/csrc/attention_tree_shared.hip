@@ -44,7 +44,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
   constexpr int CHUNKS = DP / 8, ROWS = 16 * RB * WAVES, MINE = TILE / WAVES, PER = 64 / CHUNKS, LOADS = MINE / PER;
   constexpr int SETS = RB == 1 && DP <= 128 ? 2 : 1;  // of registers for tiles on their way
   constexpr uint64_t EVERY = TILE == 64 ? ~0ull : (1ull << TILE) - 1;
-  constexpr float LAG2 = LAG_BITS - 0.05f;
+  // Plain scores are taken as powers of two while the maximum, in these units, is below 2^18.  It is rounded by itself there, and so are the maximum
+  // plus LAG2 and plus LAG_BITS: by 3 2^-7 in all, which LAG2 makes room for (no weight above 1); beyond 2^32 it would be off by more
+  // than all exponents of float32.
+  constexpr float LAG2 = LAG_BITS - 0.05f, FAST_BELOW = 0x1p18f;
   __shared__ __attribute__((aligned(1024))) char tiles[2][2][TILE * PITCH];  // [buffer][keys, values]
   __shared__ uint16_t there[2][WAVES];
   __shared__ uint64_t seen_lds[ROWS];
@@ -173,7 +176,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
     const int last_pos = d.base + d.n - 1;  // no position is beyond it
 
     // Plain scores (no cap, no slopes) are taken as powers of two at once, exp2(c2 z - m), and m is in those units too; others, and those whose
-    // powers would be beyond 2^100, keep their own units until the maximum is taken off.
+    // maximum is not below FAST_BELOW, keep their own units until the maximum is taken off.
     bool fast = PLAIN && a.scale > 0.f && c2 < 1e30f;
     float m[RB], l[RB];
     f32x4 o[RB][NDB];
@@ -280,9 +283,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
         for (int rb = 0; rb < RB; ++rb) {
           top[rb] = fmaxf(top[rb], __shfl_xor(top[rb], 16, 64));
           top[rb] = fmaxf(top[rb], __shfl_xor(top[rb], 32, 64));
-          far |= fabsf(top[rb] * c2) > 0x1p100f && top[rb] != -INFINITY;
+          const float now = fmaxf(m[rb], top[rb] * c2);
+          far |= (fabsf(now) >= FAST_BELOW && now != -INFINITY) || (m[rb] == -INFINITY && top[rb] > -INFINITY && now == -INFINITY);
         }
-        if (__builtin_expect(fast && __any(far), 0)) {  // (as far from 0 as that, what the conversion rounds is either the same or gone)
+        if (__builtin_expect(fast && __any(far), 0)) {  // (the conversion rounds a maximum as a score of its size is rounded)
           fast = false;
 #pragma unroll
           for (int rb = 0; rb < RB; ++rb) {
