@@ -291,7 +291,7 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X), RB))
         }
         // The maximum moves only when some score passes it by a factor of nearly 2^8, so that the four lanes of a row need not exchange
         // theirs.  All weights are 2^-8 of what they would be (sums, and so lse, with them): none is above 1, and no product with a
-        // finite value overflows.
+        // finite value overflows.  (The difference is compared: from 2^24 on a sum with LAG would be rounded up.)
         float top[RB];
         bool moves = false;
 #pragma unroll
@@ -301,7 +301,7 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X), RB))
           for (int st = 0; st < SUB; ++st)
 #pragma unroll
             for (int i = 0; i < 4; ++i) top[rb] = fmaxf(top[rb], z[rb][st][i]);
-          moves |= top[rb] > m[rb] + LAG;
+          moves |= top[rb] - m[rb] > LAG;
         }
         if (__builtin_expect(__any(moves), 0)) {
 #pragma unroll

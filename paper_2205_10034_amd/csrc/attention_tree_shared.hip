@@ -44,8 +44,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
   constexpr int CHUNKS = DP / 8, ROWS = 16 * RB * WAVES, MINE = TILE / WAVES, PER = 64 / CHUNKS, LOADS = MINE / PER;
   constexpr int SETS = RB == 1 && DP <= 128 ? 2 : 1;  // of registers for tiles on their way
   constexpr uint64_t EVERY = TILE == 64 ? ~0ull : (1ull << TILE) - 1;
-  // Plain scores are taken as powers of two while the maximum, in these units, is below 2^18.  It is rounded by itself there, and so are the maximum
-  // plus LAG2 and plus LAG_BITS: by 3 2^-7 in all, which LAG2 makes room for (no weight above 1); beyond 2^32 it would be off by more
+  // Plain scores are taken as powers of two while the maximum, in these units, is below 2^18.  It is rounded by itself there, and so are a score that is
+  // compared with it and its sum with LAG_BITS: by 3 2^-7 in all, which LAG2 makes room for (no weight above 1); beyond 2^32 it would be off by more
   // than all exponents of float32.
   constexpr float LAG2 = LAG_BITS - 0.05f, FAST_BELOW = 0x1p18f;
   __shared__ __attribute__((aligned(1024))) char tiles[2][2][TILE * PITCH];  // [buffer][keys, values]
@@ -274,8 +274,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
         for (int st = 0; st < SUB; ++st)
 #pragma unroll
           for (int i = 0; i < 4; ++i) top[rb] = fmaxf(top[rb], z[rb][st][i]);
-        // (a first score is always one, also where its power is beyond float32)
-        moves |= (fast ? top[rb] * c2 : top[rb]) > m[rb] + (fast ? LAG2 : LAG) || (m[rb] == -INFINITY && top[rb] > -INFINITY);
+        // (the difference, since a sum can be rounded up; a first score is always one, also where its power is beyond float32)
+        moves |= (fast ? top[rb] * c2 : top[rb]) - m[rb] > (fast ? LAG2 : LAG) || (m[rb] == -INFINITY && top[rb] > -INFINITY);
       }
       if (__builtin_expect(__any(moves), 0)) {
         bool far = false;

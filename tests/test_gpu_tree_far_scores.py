@@ -1,10 +1,10 @@
-"""Tree attention of scores far from zero: equal ones, single largest ones, and rows that differ by many orders."""
+"""Tree attention of scores far from zero: equal ones, single largest ones, rows that differ by many orders, and large values under them."""
 import numpy as np
 import pytest
 import torch
 
 from attention_util import DT, HALF_STEP, Paged, queries
-from drafts_util import attend_tree, check_tree, firsts
+from drafts_util import attend_tree, check_tree, firsts, tree_words
 from oracle import drafts_oracle as O
 
 pytestmark = pytest.mark.gpu
@@ -63,3 +63,32 @@ def test_rows_whose_scores_are_far_beside_others(D, n, G, rise):
     out, lse = attend_tree(p.cache(), q, firsts([n, n]), lens, n, scale=1.0)
     check_tree(p, q[:, 1:], firsts([n, n]), lens, n, out[:, 1:], lse[:, 1:], scale=1.0)
     check_equal_or_gone(p, q[:, :1], firsts([n, n]), lens, n, out[:, :1], lse[:, :1])
+
+
+@pytest.mark.parametrize("dtype,D,n,G,far", [("bf16", 64, 4, 2, 128), ("bf16", 128, 8, 4, 128), ("bf16", 256, 4, 2, 64), ("f32", 64, 4, 2, 64), ("f32", 256, 12, 3, 64),
+                                             ("bf16", 64, 16, 4, 128), ("bf16", 128, 16, 3, 64), ("bf16", 256, 16, 4, 64), ("bf16", 64, 16, 8, 128), ("bf16", 128, 32, 4, 64)])
+@pytest.mark.parametrize("base,more", [(0.0, 5.40625), (2.0 ** 17, 5.40625), (-2.0 ** 17, 5.40625), (2.0 ** 20, 5.375), (2.0 ** 24, 6.0), (2.0 ** 26, 8.0), (-2.0 ** 26, 8.0)])
+def test_large_values_under_rising_scores(base, more, dtype, D, n, G, far):
+    """Values near the type's largest whose keys are a little better than those of tiles before: no weight is above 1, so the mean of finite values
+    is finite.  Scores and their differences are exact; weights are off by their power's 16 units at most, sums of n by n * 2^-24."""
+    lens = [max(far + 1, n), 257, 900]
+    p = Paged(lens, 1, D, 16, dtype)
+    big = torch.tensor(3e38).to(DT[dtype]).item()
+    for s, length in enumerate(lens):
+        for j in range(length):
+            p.k[at(p, s, j)], p.v[at(p, s, j)] = 0.0, 1.0
+            p.k[at(p, s, j)][0] = base
+        p.k[at(p, s, far)][1], p.v[at(p, s, far)] = more, big
+        p.v[at(p, s, far)][1::2] = -big
+    q = torch.zeros(3 * n, G, D, dtype=DT[dtype])
+    q[:, :, :2] = 1.0
+    words = tree_words([n] * 3)
+    out, lse = attend_tree(p.cache(), q, firsts([n] * 3), lens, n, words, scale=1.0)
+    ref, ref_lse, mean_abs, *_ = O.tree(p.k, p.v, p.table, q.float().numpy(), firsts([n] * 3), lens, n, words, 1.0)
+    lost = int((~np.isfinite(out)).sum())
+    assert lost == 0, f"{lost} of {out.size} are not finite"
+    tol = (2 * (max(lens) + 64) * E + (2.0 ** -16 if dtype == "bf16" else 0.0)) * mean_abs + HALF_STEP[dtype] * 1.01 * np.abs(ref)
+    # fast units: exponents are powers of two of numbers up to 2^18, whose difference c2 = scale log2(e) scales with one rounding
+    tol += 2 * 16 * E * mean_abs
+    assert (np.abs(out - ref) <= tol).all(), f"off by {(np.abs(out - ref) / tol).max()} times what is allowed"
+    assert (np.abs(lse - ref_lse) <= 8 * E * np.abs(ref_lse) + (max(lens) + 64) * E).all()
