@@ -244,7 +244,7 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X), RB))
         entry = entry_next;
         load_keys();
         // Scores stay in their own units until the maximum is taken off: in powers of two those beyond 2.4e38 would be infinite.
-        const bool with_drafts = p0 + TILE > d.base;
+        const bool with_drafts = p0 > d.base - TILE;
         if (plain) {
 #pragma unroll
           for (int rb = 0; rb < RB; ++rb)
@@ -268,7 +268,7 @@ __global__ __launch_bounds__(64 * WAVES, resident_workgroups(DP, sizeof(X), RB))
         }
         // Everyone sees everything of a tile that is all there, before the new tokens, and in the window of the last position or among
         // the sinks.
-        const bool masked = here != EVERY || with_drafts || (a.window > 0 && last_pos - p0 >= a.window && p0 + TILE > a.sinks);
+        const bool masked = here != EVERY || with_drafts || (a.window > 0 && last_pos - p0 >= a.window && p0 > a.sinks - TILE);
         uint32_t seen_here = 0;  // places that this lane's rows see, 4 SUB bits to a row
         if (__builtin_expect(masked, 0)) {
           uint64_t seen[RB];

@@ -238,7 +238,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
           for (int i = 0; i < 4; ++i) {
             const int p = p0 + st * 16 + g * 4 + i;
             int pos_p = p;
-            if (p0 + TILE > d.base && p >= d.base) pos_p = d.base + depth_lds[p - d.base < MOE_MAX_DRAFTS ? p - d.base : 0];
+            if (p0 > d.base - TILE && p >= d.base) pos_p = d.base + depth_lds[p - d.base < MOE_MAX_DRAFTS ? p - d.base : 0];
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
               float s = z[rb][st][i] * a.scale;
@@ -432,7 +432,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void shared_kernel(TreeArgs a) {
       const int p0 = span.tile(u) * TILE;
       // Everyone sees everything of a tile that is all there, before the new tokens, and in the window of the last position or among
       // the sinks.
-      const bool masked = here != EVERY || p0 + TILE > d.base || (a.window > 0 && last_pos - p0 >= a.window && p0 + TILE > a.sinks);
+      const bool masked = here != EVERY || p0 > d.base - TILE || (a.window > 0 && last_pos - p0 >= a.window && p0 > a.sinks - TILE);
       if (__builtin_expect(masked, 0)) without_odd_values(p0, BUFFER, here);
       if (active) compute(p0, BUFFER, here, masked, key);
       __builtin_amdgcn_sched_barrier(0);
