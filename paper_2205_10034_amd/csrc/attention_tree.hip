@@ -545,7 +545,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(TreeArgs a) {
 struct Split {
   int blocks, rows, row_tiles, items, parts, small;
   bool shared, nt, may_split;
-  size_t ml, o, total;  // bytes: offsets of the pieces (the plan lies in front)
+  size_t ml, o, total;  // bytes: offsets of the pieces (the plan lies in front); enough for fewer new tokens too, as far as `rows` is the same
 };
 
 Split split_of(const moe_kv_cache* c, int32_t n_q_heads, int32_t max_new, int32_t window, int32_t sinks) {
@@ -567,6 +567,8 @@ Split split_of(const moe_kv_cache* c, int32_t n_q_heads, int32_t max_new, int32_
   const int least = s.shared ? 256 : (es == 2 && dims <= 128 ? 32 : 16) * LEAST;  // places of a part
   const int64_t most = (int64_t)c->n_seqs * ((capacity + least - 1) / least);  // pieces of work there can be
   if (parts > most) parts = most > 1 ? most : 1;
+  int64_t most_slots = 2 * s.rows * (resident > s.items ? resident : s.items);  // of this call or one of fewer items
+  if (most_slots > 2 * s.rows * most * s.items) most_slots = 2 * s.rows * most * s.items;
   if (!s.may_split) parts = c->n_seqs;
   s.parts = (int)parts;
   // Pools that the last-level cache (256 MB) cannot keep for the next call are read past it, where one workgroup reads them.
@@ -574,7 +576,8 @@ Split split_of(const moe_kv_cache* c, int32_t n_q_heads, int32_t max_new, int32_
   const int64_t slots = s.may_split ? 2 * parts * s.items * s.rows : 0;
   s.ml = align_up((size_t)c->n_seqs * s.row_tiles * sizeof(int2), 256);
   s.o = s.ml + align_up((size_t)slots * sizeof(f32x2), 256);
-  s.total = s.o + align_up((size_t)slots * c->head_dim * sizeof(float), 256);
+  if (!s.may_split || most_slots < slots) most_slots = slots;
+  s.total = s.ml + align_up((size_t)most_slots * sizeof(f32x2), 256) + align_up((size_t)most_slots * c->head_dim * sizeof(float), 256);
   if (s.total < 256) s.total = 256;
   return s;
 }
@@ -632,7 +635,15 @@ extern "C" size_t moe_attention_tree_workspace_bytes(const moe_kv_cache* c, int3
     fail(MOE_ERR_INVALID_ARG, "max_new=%d outside 1..%d", max_new, MOE_MAX_DRAFTS);
     return 0;
   }
-  return split_of(c, n_q_heads, max_new, 0, 0).total;
+  // a larger call's workspace serves a smaller one: the most that any number of new tokens up to max_new wants
+  size_t total = split_of(c, n_q_heads, max_new, 0, 0).total;
+  for (int rows = 16; rows <= 64; rows *= 2) {  // (up to which the rows of a workgroup are the same)
+    const int fewer = rows / (n_q_heads / c->n_kv_heads);
+    if (fewer < 1 || fewer >= max_new) continue;
+    const size_t less = split_of(c, n_q_heads, fewer, 0, 0).total;
+    total = less > total ? less : total;
+  }
+  return total;
 }
 
 extern "C" int32_t moe_attention_tree(const moe_kv_cache* c, int32_t n_q_heads, int32_t T, int32_t max_new, const moe_head_rows* q,

@@ -631,30 +631,39 @@ __global__ __launch_bounds__(64 * TEAM) void select_kernel(RowArgs a) {
   if (lane < a.K) store(lane, keys[lane]);
 }
 
-// How a call's rows are divided.
+// How a call's rows are divided; groups' maxima begin `groups` bytes into the workspace.
+constexpr int MOST_PARTS = 2048;  // of rows that are split
 struct Division {
   int team, parts, part_chunks, max_chunks;
-  size_t groups, total;  // bytes
+  size_t groups;
 };
+bool splits(int chunks, int K) { return chunks > (K > 0 ? 16 : 64); }
+int most_parts(int chunks) { return (chunks + 7) / 8; }  // of a row
 Division division_of(int T, int V, int K) {
   const int chunks = most_chunks(V, 16, 2);
-  Division d{chunks <= 2 ? 1 : WAVES, 1, chunks, chunks, 0, 256};
+  Division d{chunks <= 2 ? 1 : WAVES, 1, chunks, chunks, 0};
   // Without alternatives, whose kernel joins the parts as well, a split costs a launch: rows of up to 65536 logits, and 256 of
   // any length, are faster whole (us, split / whole: 1 row of 50001 bfloat16 logits 11.8 / 8.2, of 250000 11.0 / 19.0; 200 of 250000 22.5 / 26.9; 300 of 128000
   // 18.1 / 16.8; 1000 float32 rows of 32003 26.8 / 24.0).
-  if (chunks > 16 && (K > 0 || (T < 256 && chunks > 64))) {
-    int64_t parts = T > 0 ? 2048 / T : 1;
-    const int64_t most = (chunks + 7) / 8;
-    if (parts > most) parts = most;
+  if (splits(chunks, K) && (K > 0 || T < 256)) {
+    int parts = T > 0 ? MOST_PARTS / T : 1;
+    if (parts > most_parts(chunks)) parts = most_parts(chunks);
     if (parts < 1) parts = 1;
-    d.part_chunks = (int)((chunks + parts - 1) / parts);
+    d.part_chunks = (chunks + parts - 1) / parts;
     d.part_chunks = (d.part_chunks + WAVES - 1) / WAVES * WAVES;
     d.parts = (chunks - 1) / d.part_chunks + 1;
   }
-  if (d.parts > 1 || K > 0) d.total = d.groups = align_up((size_t)T * d.parts * sizeof(f32x4), 256);
-  if (K > 0) d.total += (size_t)T * chunks * 64 * sizeof(uint32_t);
-  if (d.total < 256) d.total = 256;
+  d.groups = align_up((size_t)T * d.parts * sizeof(f32x4), 256);
   return d;
+}
+
+// What division_of wants for T rows and for any fewer: T parts, or as many more as rows are split into.
+size_t workspace_of(int T, int V, int K) {
+  const int chunks = most_chunks(V, 16, 2);
+  const int64_t split = (int64_t)T * most_parts(chunks), parts = !splits(chunks, K) ? 0 : split < MOST_PARTS ? split : MOST_PARTS;
+  size_t total = align_up((size_t)(K > 0 && T > parts ? T : parts) * sizeof(f32x4), 256);
+  if (K > 0) total += (size_t)T * chunks * 64 * sizeof(uint32_t);
+  return total < 256 ? 256 : total;
 }
 
 template <typename X, bool ENTROPY, bool TOP>
@@ -795,7 +804,7 @@ extern "C" size_t moe_token_logprobs_workspace_bytes(int32_t T, int32_t V, int32
     fail(MOE_ERR_INVALID_ARG, "T=%d must not be negative, V=%d at least 1, K=%d in 0..min(V, %d)", T, V, K, MOE_MAX_ALTERNATIVES);
     return 0;
   }
-  return division_of(T, V, K).total;
+  return workspace_of(T, V, K);
 }
 
 extern "C" int32_t moe_token_logprobs(int32_t dtype, int32_t T, int32_t V, const void* x, int64_t row_stride, float scale,
