@@ -183,19 +183,6 @@ struct TopList {
       bound = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(bound >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)bound);
     }
   }
-
-  // A key of each lane that has one.
-  __device__ __forceinline__ void offer(bool have, uint64_t key) {
-    unsigned long long all = __ballot(have && key > bound);
-    if (!all) return;
-    if (n + __popcll(all) > LIST) {
-      sort();
-      all = __ballot(have && key > bound);
-    }
-    if (have && key > bound) keys[n + __popcll(all & ((1ull << (threadIdx.x & 63)) - 1))] = key;
-    n += __popcll(all);
-    asm volatile("" ::: "memory");
-  }
 };
 
 // A value that K of the lanes' (N each, 0: no value) reach: the K-th largest, cut down to the upper BITS bits; 0 where there are fewer.
