@@ -727,8 +727,11 @@ int32_t moe_token_logprobs(int32_t dtype, int32_t T, int32_t V, const void* x, i
  *   d_x_j = scale*(d_logp ([j = id] - p_j) - d_entropy p_j (log p_j + entropy) + d_lse p_j),  rounded once to dtype.
  * d_logp of a token outside 0..V-1 is not used.  A row whose three factors are all 0, or whose lse is -infinity, has
  * gradient 0 whatever its logits are; a logit of -infinity has gradient 0 (d_logp*scale where it is the token's own).
- * p carries lse's own rounding, 2^-24 |lse| of it; where |lse| is above 1024 (MOE_F32: 64; a row of the type's lowest value, say) the row's sum is taken anew.
- * d_x [T, V], d_row_stride >= V elements apart; may be x itself with x's stride (row_stride >= V then), and must not overlap it otherwise. */
+ * p carries lse's own rounding, 2^-24 |lse| of it.  What that does not tell is taken from the row again: its sum where |lse| is above 1024
+ * (MOE_F32: 64; a row of the type's lowest value, say), and for a token that is nearly certain 1 - p, which has 11 bits at least (MOE_F32: 17)
+ * whatever lse is; such rows take longer.
+ * d_x [T, V], d_row_stride >= V elements apart; may be x itself with x's stride (row_stride >= V then; a row is one workgroup's then, which is
+ * slower where rows are few), and must not overlap it otherwise. */
 int32_t moe_token_logprobs_backward(int32_t dtype, int32_t T, int32_t V, const void* x, int64_t row_stride, float scale,
                                     const int32_t* ids, const float* lse, const float* d_logp, const float* entropy,
                                     const float* d_entropy, const float* d_lse, void* d_x, int64_t d_row_stride,

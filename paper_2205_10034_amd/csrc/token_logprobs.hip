@@ -22,8 +22,10 @@ constexpr int LIST = 128;                            // candidates that a wavefr
 constexpr int FOUND = 512;                           // groups with candidates that a row's workgroup holds
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float LAG_BITS = 8.f;
-// Where lse's rounding shows in p: 2^-14 of it there in bfloat16 (a gradient is rounded to 2^-9), 2^-18 in float32.
+// lse's rounding is 2^-24 |lse| of every p.  The gradient leaves it there up to 2^-14 of p in bfloat16 (which is rounded to 2^-9), 2^-18 in float32:
 template <typename X> constexpr float far_lse = sizeof(X) == 2 ? 1024.f : 64.f;
+// ... and, of 1 - p and log p of a token that is nearly certain, up to 2^-11 and 2^-17 of these (8: what s and the power carry, in the same units).
+template <typename X> __device__ __forceinline__ float near_certain(float lse) { return (fabsf(lse) + 8.f) * (sizeof(X) == 2 ? 0x1p-13f : 0x1p-7f); }
 
 // 16 bytes of logits at any alignment of their elements
 template <typename X> struct __attribute__((packed, aligned(sizeof(X)))) Unaligned {
@@ -51,10 +53,10 @@ template <typename X> constexpr uint32_t minus_infinities = sizeof(X) == 2 ? 0xf
 template <typename X>
 __device__ __forceinline__ u32x4 load_some(const X* x, int64_t j, int V) {
   if (j >= 0 && j + per_load<X> <= V) return reinterpret_cast<const Unaligned<X>*>(x + j)->v;
-  u32x4 v;
+  u32x4 v{minus_infinities<X>, minus_infinities<X>, minus_infinities<X>, minus_infinities<X>};
+  if (j >= V) return v;
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
-    v[w] = minus_infinities<X>;
     if constexpr (sizeof(X) == 2) {
       const int64_t k = j + 2 * w;
       if (k >= 0 && k < V) v[w] = (v[w] & 0xffff0000u) | reinterpret_cast<const uint16_t*>(x)[k];
@@ -677,13 +679,15 @@ int32_t launch_rows(const RowArgs& a, const Division& d, hipStream_t s) {
 
 // ---- backward ------------------------------------------------------------------------------------------
 
+constexpr int LARGE_TEAM = 16;
+
 struct GradArgs {
   const char* x;
   char* d_x;
   int64_t row_stride, d_row_stride;  // bytes
   const int32_t* ids;
   const float *lse, *d_logp, *entropy, *d_entropy, *d_lse;
-  int32_t T, V, parts, part_chunks, line;
+  int32_t T, V, groups, group_chunks, line, in_place, one_takes_all, owner_shift;
   float scale, c, lag;
 };
 
@@ -707,6 +711,7 @@ __device__ __forceinline__ void store_some(X* x, int64_t j, int V, const u32x4& 
     __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(x + j));
     return;
   }
+  if (j >= V) return;  // (most lanes of a short row)
 #pragma unroll
   for (int e = 0; e < per_load<X>; ++e) {
     if (j + e < 0 || j + e >= V) continue;
@@ -715,63 +720,224 @@ __device__ __forceinline__ void store_some(X* x, int64_t j, int V, const u32x4& 
   }
 }
 
-// A wavefront to a part of a row, the rows from the last one on (the forward call has read that one last).
+// -infinity in the place of element e
+__device__ __forceinline__ void forget(const __bf16*, u32x4& v, int e) { v[e / 2] = e & 1 ? (v[e / 2] & 0xffffu) | 0xff800000u : (v[e / 2] & 0xffff0000u) | 0xff80u; }
+__device__ __forceinline__ void forget(const float*, u32x4& v, int e) { v[e] = 0xff800000u; }
+
+// Element `at` of a wavefront's chunk, for all its lanes.
 template <typename X>
-__global__ __launch_bounds__(THREADS) void gradient_kernel(GradArgs a) {
-  const unsigned units = (unsigned)a.T * (unsigned)a.parts, unit = blockIdx.x * WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+__device__ __forceinline__ float pick(const X* kind, const u32x4 (&v)[loads<X>], int at) {
+  constexpr int N = per_load<X>;
+  const int l_at = at / (64 * N), w_at = at % N / (N / 4);
+  auto choose = [](int which, uint32_t a, uint32_t b) { return (a & ((uint32_t)which - 1u)) | (b & (0u - (uint32_t)which)); };  // 0 or 1
+  auto word_of = [&](int w) {
+    const uint32_t lower = choose(l_at & 1, v[0][w], v[1][w]);
+    if constexpr (loads<X> == 2) return lower;
+    else return choose(l_at >> 1 & 1, lower, choose(l_at & 1, v[loads<X> - 2][w], v[loads<X> - 1][w]));
+  };
+  uint32_t word = choose(w_at >> 1 & 1, choose(w_at & 1, word_of(0), word_of(1)), choose(w_at & 1, word_of(2), word_of(3)));
+  word = (uint32_t)__builtin_amdgcn_readlane((int)word, at / N & 63);
+  return element(kind, u32x4{word, word, word, word}, at % (N / 4));
+}
+
+// TEAM wavefronts to one of a row's `groups`, chunk after chunk in turn, the rows from the last one on (the forward call has read that one last).
+//   d_j = scale p_j (gl - g - ge (log p_j + h)),  and scale g more for the token itself, log p_j = scale x_j - lse.
+// What lse does not tell well enough is taken from the row again, before anything is written (x may be y):
+//  - Of rows far from zero (far_lse), and of the entropy's gradient where nearly all is one token's, the sum.  One group does the whole row; of
+//    few rows every group the sum for itself.
+//  - Of a token that is nearly certain r = sum_{j != id} p_j, by the group that has it: 1 - p without a difference, and log p = log(1 - r).
+// REGISTERS: a row has TEAM chunks or fewer, nothing is read twice.
+// Bound: HBM (8192 rows of 50001 bfloat16 logits 262 us, 6.2 TB/s read + written); of rows that are read again also the vector unit, for exp.  us of
+// usual rows / rows whose token has all but 1e-4 / rows far from zero:  8192 of 50001 bfloat16 262 / 350 / 434, 1000 of 32003 float32 40 / 55 / 80,
+// 1 of 262144 float32 9 / 18 / 21, 16384 of 1000 bfloat16 13 / 20 / 20.  In place: 329, 41, 26, 13 of usual ones, since a row is one group's.
+template <typename X, int TEAM, bool REGISTERS>
+__global__ __launch_bounds__(TEAM > WAVES ? 64 * TEAM : THREADS) void gradient_kernel(GradArgs a) {
+  constexpr int BLOCK = TEAM > WAVES ? TEAM : WAVES;
+  __shared__ Stats stats[BLOCK];
+  __shared__ float id_lds;
+  const X* kind = nullptr;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), me = wave % TEAM;
+  const unsigned units = (unsigned)a.T * (unsigned)a.groups, unit = blockIdx.x * (BLOCK / TEAM) + wave / TEAM;
   if (unit >= units) return;
-  const int t = (int)((units - 1 - unit) / (unsigned)a.parts), part = (int)((units - 1 - unit) - (unsigned)t * (unsigned)a.parts);
+  const int t = (int)((units - 1 - unit) / (unsigned)a.groups), group = (int)((units - 1 - unit) - (unsigned)t * (unsigned)a.groups);
   const X* x = reinterpret_cast<const X*>(a.x + (int64_t)t * a.row_stride);
   X* y = reinterpret_cast<X*>(a.d_x + (int64_t)t * a.d_row_stride);
-  const int back = elements_behind(y, a.line), all_chunks = (int)(((int64_t)a.V + back - 1) / CHUNK) + 1, c0 = part * a.part_chunks, c1 = c0 + a.part_chunks < all_chunks ? c0 + a.part_chunks : all_chunks;
-  const int id = a.ids ? a.ids[t] : -1;
-  const float lse = a.lse[t], g = a.d_logp && (unsigned)id < (unsigned)a.V ? a.d_logp[t] : 0.f, ge = a.d_entropy ? a.d_entropy[t] : 0.f, gl = a.d_lse ? a.d_lse[t] : 0.f;
-  if (lse == -INFINITY || (g == 0.f && ge == 0.f && gl == 0.f)) {
-    for (int c = c0; c < c1; ++c)
+  const int back = elements_behind(y, a.line), all_chunks = (int)(((int64_t)a.V + back - 1) / CHUNK) + 1;
+  int c0 = group * a.group_chunks, c1 = c0 + a.group_chunks < all_chunks ? c0 + a.group_chunks : all_chunks;
+  auto inside = [&](int c) { return !(REGISTERS && TEAM == 1) && (c > 0 || back == 0) && (int64_t)(c + 1) * CHUNK - back <= a.V; };  // the whole chunk is the row's
+  auto load = [&](int c, u32x4 (&v)[loads<X>]) {  // (nothing of chunks behind the last)
+    if (inside(c)) {
+      load_chunk(x + ((int64_t)c * CHUNK - back), v);
+    } else {
 #pragma unroll
-      for (int l = 0; l < loads<X>; ++l) store_some(y, index_of<X>(c, l, threadIdx.x & 63, back), a.V, u32x4{0, 0, 0, 0});
+      for (int l = 0; l < loads<X>; ++l) v[l] = load_some(x, index_of<X>(c, l, lane, back), a.V);
+    }
+  };
+  int id = a.ids ? a.ids[t] : -1;
+  const float lse = a.lse[t], ge = a.d_entropy ? a.d_entropy[t] : 0.f, gl = a.d_lse ? a.d_lse[t] : 0.f;
+  float h = a.d_entropy ? a.entropy[t] : 0.f, g = a.d_logp ? a.d_logp[t] : 0.f;
+  u32x4 v[loads<X>];
+  load(c0 + me, v);
+  if ((unsigned)id >= (unsigned)a.V || !a.d_logp) id = -1;
+  if (id < 0) g = 0.f;
+  if (ge == 0.f) h = 0.f;
+  // the token's own logit, where it is this group's (in place the whole row is)
+  const int id_chunk = (int)(((int64_t)id + back) / CHUNK);
+  bool has_id = id >= 0 && id_chunk >= c0 && id_chunk < c1;
+  float id_logit = 0.f;
+  if (lse == -INFINITY || (g == 0.f && ge == 0.f && gl == 0.f)) {
+    for (int c = c0 + me; c < c1; c += TEAM)
+#pragma unroll
+      for (int l = 0; l < loads<X>; ++l) store_some(y, index_of<X>(c, l, lane, back), a.V, u32x4{0, 0, 0, 0});
     return;
   }
-  const float h = ge != 0.f ? a.entropy[t] : 0.f;
-  // log p_j = (x_j - m) scale - log_s: with lse as it is, unless that is so large that its rounding shows in p (a mask of the type's lowest
-  // value that leaves nothing).  One wavefront has all of such a row then, whose sum it takes again before it writes (x may be y).
-  float m = 0.f, log_s = lse;
-  int from = c0, upto = c1;
-  if (fabsf(lse) > far_lse<X>) {
-    if (part != 0) return;
-    Stats st{-INFINITY, 0.f, 0.f};
-    upto = all_chunks;
-    for (int c = 0; c < all_chunks; ++c) {
-      u32x4 v[loads<X>];
-#pragma unroll
-      for (int l = 0; l < loads<X>; ++l) v[l] = load_some(x, index_of<X>(c, l, threadIdx.x & 63, back), a.V);
-      take_chunk<X, false>(st, v, a.c, a.lag);
+  if (g == 0.f) {
+    id = -1;
+    has_id = false;
+  }
+  if (has_id && id_chunk - c0 < TEAM) {  // a wavefront has it in registers
+    if (id_chunk == c0 + me) {
+      id_logit = pick(kind, v, (int)((int64_t)id + back - (int64_t)id_chunk * CHUNK));
+      if (TEAM > 1 && lane == 0) id_lds = id_logit;
     }
+    if (TEAM > 1) {
+      lds_barrier();
+      id_logit = id_lds;
+    }
+  } else if (has_id) {
+    id_logit = (float)x[id];
+    if (a.in_place) {
+      asm volatile("" : "+v"(id_logit));  // it has arrived
+      lds_barrier();                      // ... everywhere, before its place is written
+    }
+  }
+  const float near = near_certain<X>(lse);
+  const bool whole_row = fabsf(lse) > far_lse<X> || (ge != 0.f && fabsf(h) < near);
+  if (whole_row && a.one_takes_all) {
+    if (group != (t >> a.owner_shift) % a.groups) return;  // (the same of all rows would lie on one die)
+    if (c0) load(me, v);
+    c0 = 0;
+    c1 = all_chunks;
+  }
+  float m = 0.f, log_s = lse, own = 0.f;
+  bool certain = false;  // the token's own element is `own`
+  // All of the row but the token's own logit, GULP chunks at a time.
+  auto for_others = [&](auto take) {
+    constexpr int GULP = REGISTERS ? 1 : 2;
+#pragma unroll 1
+    for (int c = me; c < all_chunks; c += GULP * TEAM) {
+      u32x4 w[GULP][loads<X>];
+#pragma unroll
+      for (int i = 0; i < GULP; ++i) {
+        if constexpr (REGISTERS) {
+#pragma unroll
+          for (int l = 0; l < loads<X>; ++l) w[i][l] = v[l];
+        } else {
+          load(c + i * TEAM, w[i]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < GULP; ++i) {
+        if (id >= 0 && id_chunk == c + i * TEAM) {
+          const int at = (int)((int64_t)id + back - (int64_t)id_chunk * CHUNK);
+#pragma unroll
+          for (int l = 0; l < loads<X>; ++l)
+#pragma unroll
+            for (int e = 0; e < per_load<X>; ++e)
+              if (first_of<X>(l) + e == at) forget(kind, w[i][l], e);
+        }
+        take(w[i]);
+      }
+    }
+  };
+  if (__builtin_expect(whole_row, 0)) {
+    if (id >= 0 && !has_id) id_logit = (float)x[id];  // (not in place)
+    Stats st{-INFINITY, 0.f, 0.f};
+    for_others([&](const u32x4 (&w)[loads<X>]) { take_chunk<X, false>(st, w, a.c, a.lag); });
     join_lanes<false>(st, a.c);
     m = st.m;
-    log_s = logf(st.s);
-  }
-  // d_j = p_j (gl - g - ge (log p_j + h)) scale, and g scale more for the token itself
-  const float flat = a.scale * (gl - g - ge * h), steep = -a.scale * ge, own = a.scale * g;
-  for (int c = from; c < upto; ++c) {
-    u32x4 v[loads<X>];
+    if (TEAM > 1) {
+      if (lane == 0) stats[wave] = st;
+      lds_barrier();  // (the whole row has been read: x may be y)
 #pragma unroll
-    for (int l = 0; l < loads<X>; ++l) v[l] = load_some(x, index_of<X>(c, l, threadIdx.x & 63, back), a.V);
+      for (int w = 0; w < TEAM; ++w) m = fmaxf(m, stats[w].m);
+      st = Stats{m, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < TEAM; ++w) {
+        Stats other = stats[w];
+        refer<false>(other, m, a.c);
+        st.s += other.s;
+      }
+    }
+    float p = 0.f;
+    if (id >= 0) {
+      m = fmaxf(m, id_logit);
+      refer<false>(st, m, a.c);
+      p = __builtin_amdgcn_exp2f((id_logit - m) * a.c);
+    }
+    const float s = st.s + p, rest = st.s / s;
+    log_s = logf(s);
+    const float lp = p > st.s ? log1pf(-rest) : (id_logit - m) * a.scale - log_s;
+    own = a.scale * (g * rest + (p == 0.f ? 0.f : p / s * (gl - ge * (lp + h))));
+    certain = true;
+  } else if (has_id && __builtin_fmaf(id_logit, a.scale, -lse) > -near) {
+    float rest = 0.f;
+    for_others([&](const u32x4 (&w)[loads<X>]) {
+#pragma unroll
+      for (int l = 0; l < loads<X>; ++l)
+#pragma unroll
+        for (int e = 0; e < per_load<X>; ++e) rest += __builtin_amdgcn_exp2f(__builtin_fmaf(element(kind, w[l], e), a.scale, -lse) * LOG2E);
+    });
+#pragma unroll
+    for (int d = 32; d; d >>= 1) rest += __shfl_xor(rest, d, 64);
+    if (TEAM > 1) {
+      if (lane == 0) stats[wave].s = rest;
+      lds_barrier();
+      rest = 0.f;
+#pragma unroll
+      for (int w = 0; w < TEAM; ++w) rest += stats[w].s;
+    }
+    own = a.scale * (g * rest + (1.f - rest) * (gl - ge * (log1pf(-rest) + h)));
+    certain = true;
+  }
+  const float flat = a.scale * (gl - g - ge * h), steep = -a.scale * ge;
+  for (int c = c0 + me; c < c1; c += TEAM) {
+    const bool all = inside(c);
+    X* to = y + ((int64_t)c * CHUNK - back);
+    const int id_here = id >= 0 && id_chunk == c ? (int)((int64_t)id + back - (int64_t)c * CHUNK) : -1;
 #pragma unroll
     for (int l = 0; l < loads<X>; ++l) {
-      const int64_t j = index_of<X>(c, l, threadIdx.x & 63, back);
+      const int first = first_of<X>(l);
       float d[per_load<X>];
 #pragma unroll
       for (int e = 0; e < per_load<X>; ++e) {
-        const float lp = __builtin_fmaf(element((const X*)nullptr, v[l], e) - m, a.scale, -log_s), p = __builtin_amdgcn_exp2f(lp * LOG2E);
+        const float lp = __builtin_fmaf(element(kind, v[l], e) - m, a.scale, -log_s), p = __builtin_amdgcn_exp2f(lp * LOG2E);
         d[e] = p == 0.f ? 0.f : p * __builtin_fmaf(steep, lp, flat);
-        if ((int)j + e == id) d[e] += own;
       }
+      if (id_here >= 0)
+#pragma unroll
+        for (int e = 0; e < per_load<X>; ++e)
+          if (first + e == id_here) d[e] = certain ? own : d[e] + a.scale * g;
       u32x4 out;
       put(d, out);
-      store_some(y, j, a.V, out);
+      if (all) __builtin_nontemporal_store(out, reinterpret_cast<u32x4*>(to + first));
+      else store_some(y, index_of<X>(c, l, lane, back), a.V, out);
     }
+    if (c + TEAM < c1) load(c + TEAM, v);
   }
+}
+
+template <typename X, int TEAM>
+void launch_gradient(const GradArgs& a, bool registers, unsigned grid, hipStream_t s) {
+  const dim3 threads(TEAM > WAVES ? 64 * TEAM : THREADS);
+  if (TEAM <= WAVES && registers) hipLaunchKernelGGL((gradient_kernel<X, TEAM, TEAM <= WAVES>), dim3(grid), threads, 0, s, a);
+  else hipLaunchKernelGGL((gradient_kernel<X, TEAM, false>), dim3(grid), threads, 0, s, a);
+}
+template <typename X>
+void launch_gradient(const GradArgs& a, int team, bool registers, unsigned grid, hipStream_t s) {
+  if (team == 1) launch_gradient<X, 1>(a, registers, grid, s);
+  else if (team == WAVES) launch_gradient<X, WAVES>(a, registers, grid, s);
+  else launch_gradient<X, LARGE_TEAM>(a, registers, grid, s);
 }
 
 int32_t check_rows(int32_t dtype, int32_t T, int32_t V, float scale, const char* who) {
@@ -831,17 +997,29 @@ extern "C" int32_t moe_token_logprobs_backward(int32_t dtype, int32_t T, int32_t
   if (d_entropy && !entropy) return fail(MOE_ERR_INVALID_ARG, "%s: d_entropy without entropy", who);
   if (row_stride < 0 || (T > 1 && d_row_stride < V)) return fail(MOE_ERR_INVALID_ARG, "%s: rows of d_x overlap, or row_stride is negative", who);
   if (T > 1 && x == d_x && row_stride != d_row_stride) return fail(MOE_ERR_INVALID_ARG, "%s: in place, d_x must have x's stride", who);
-  // Stores of whole lines: 284 against 317 us for 8192 rows of 50001 bfloat16 logits.  Short rows, which a few more elements
-  // can cost another chunk, begin on 16 bytes (16384 rows of 1000: 15 against 19 us).
+  // Stores of whole lines: a tenth of the time of 8192 rows of 50001 bfloat16 logits.  Short rows, which a few more elements can cost
+  // another chunk, begin on 16 bytes (16384 rows of 1000: a fifth).
   const int line = V > 8 * CHUNK ? 128 : 16, chunks = most_chunks(V, line, (int)es);
-  int per = chunks < 4 ? chunks : 4;
-  if ((int64_t)T * ((chunks - 1) / per + 1) < 4096) per = 1;
-  const int parts = (chunks - 1) / per + 1;
-  const int64_t grid = ((int64_t)T * parts + WAVES - 1) / WAVES;
-  if (!launchable(grid, THREADS)) return fail(MOE_ERR_UNSUPPORTED, "%s: %d rows are too many for one call", who, T);
+  // A chunk to each wavefront of a group, in place the whole row to a group.  Rows of one chunk are a wavefront's own, and so are many rows of up to four
+  // (4096 of 3000: 10.3 against 13.7 us); sixteen wavefronts take the rest of a row again sooner than four do, where few rows leave
+  // the machine idle behind them (1000 float32 rows of 32003, all of them certain: 55 against 61 us, usual ones 40 for both).
+  const bool in_place = x == d_x;
+  const int team = chunks == 1 || (chunks <= WAVES && T >= 4096) ? 1 : T < 2048 && chunks > LARGE_TEAM ? LARGE_TEAM : WAVES;
+  const int threads = team > WAVES ? 64 * team : THREADS;
+  int group_chunks = in_place || team == 1 ? chunks : team, groups = (chunks - 1) / group_chunks + 1;
+  while (groups > 1 && !launchable((int64_t)T * groups, threads)) {
+    group_chunks *= 2;
+    groups = (chunks - 1) / group_chunks + 1;
+  }
+  // Rows far from zero, one group's alone / every group's: 700 float32 ones of 100003 171 / 355 us, 64 bfloat16 ones of 128000 79 / 34.
+  const bool one_takes_all = T >= 128;
+  // (workgroups go to the eight dies in turn; the groups that take whole rows are to lie on all of them)
+  const int owner_shift = groups % 8 == 0 ? 0 : groups % 4 == 0 ? 1 : groups % 2 == 0 ? 2 : 3;
+  const int64_t grid = team == 1 ? ((int64_t)T + WAVES - 1) / WAVES : (int64_t)T * groups;
+  if (!launchable(grid, threads)) return fail(MOE_ERR_UNSUPPORTED, "%s: %d rows are too many for one call", who, T);
   const float c = fminf(scale * LOG2E, FLT_MAX);
-  const GradArgs a{(const char*)x, (char*)d_x, row_stride * (int64_t)es, d_row_stride * (int64_t)es, ids, lse, d_logp, entropy, d_entropy, d_lse, T, V, parts, per, line, scale, c, LAG_BITS / c};
-  if (dtype == MOE_BF16) hipLaunchKernelGGL(gradient_kernel<__bf16>, dim3((unsigned)grid), dim3(THREADS), 0, (hipStream_t)stream, a);
-  else hipLaunchKernelGGL(gradient_kernel<float>, dim3((unsigned)grid), dim3(THREADS), 0, (hipStream_t)stream, a);
+  const GradArgs a{(const char*)x, (char*)d_x, row_stride * (int64_t)es, d_row_stride * (int64_t)es, ids, lse, d_logp, entropy, d_entropy, d_lse, T, V, groups, group_chunks, line, in_place, one_takes_all, owner_shift, scale, c, LAG_BITS / c};
+  if (dtype == MOE_BF16) launch_gradient<__bf16>(a, team, chunks <= team, (unsigned)grid, (hipStream_t)stream);
+  else launch_gradient<float>(a, team, chunks <= team, (unsigned)grid, (hipStream_t)stream);
   return check_hip(hipGetLastError(), "log-probabilities gradient launch");
 }
