@@ -682,7 +682,7 @@ int32_t moe_kv_compact(const moe_kv_cache* c, const int32_t* base, int32_t width
 /* Pages by counts: refs (device int32 [n_pages]) says how many entries of the page table name each page; one with count 0
  * is free.  The three calls below change the cache's page table and refs together, and keep that true.  Where pages are wanted the
  * lowest free ones are given, in order; missing (nullable, device int32 [1]) becomes the number of those wanted that were
- * not to be had, whose entries stay as pages that are not there (-1).  A negative length is that of a sequence that is
+ * not to be had (INT32_MAX for more), whose entries stay as pages that are not there (-1).  A negative length is that of a sequence that is
  * not there.  Order on one stream; one call at a time on a table. */
 
 /* Pages of the places from lens[s] on (device int32 [n_seqs]; <= 0: all) are given back, their entries become -1. */

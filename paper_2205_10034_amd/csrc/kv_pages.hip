@@ -161,18 +161,19 @@ __global__ __launch_bounds__(THREADS) void share_kernel(PoolArgs a) {
 }
 
 // This thread's part of a sum in front of it, and the sum of all (GIVE_THREADS threads).
-__device__ __forceinline__ int sum_before(int mine, int& all) {
-  __shared__ int waves[GIVE_THREADS / 64];
+template <typename N>
+__device__ __forceinline__ N sum_before(N mine, N& all) {
+  __shared__ N waves[GIVE_THREADS / 64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int upto = mine;
+  N upto = mine;
   for (int d = 1; d < 64; d <<= 1) {
-    const int other = __shfl_up(upto, d, 64);
+    const N other = __shfl_up(upto, d, 64);
     if (lane >= d) upto += other;
   }
   __syncthreads();
   if (lane == 63) waves[wave] = upto;
   __syncthreads();
-  int before = upto - mine;
+  N before = upto - mine;
   all = 0;
   for (int w = 0; w < GIVE_THREADS / 64; ++w) {
     if (w < wave) before += waves[w];
@@ -208,7 +209,7 @@ __device__ __forceinline__ int take_pages(const PoolArgs& a, int wanted, uint32_
     const int64_t p = p0 + threadIdx.x * PER;
     if (p0) free = free_pages(a, p);
     int all;
-    int rank = found + sum_before(__popc(free), all);
+    int rank = found + sum_before<int>(__popc(free), all);
     for (; free && rank < wanted; free &= free - 1, ++rank) {
       const int page = (int)(p + __ffs(free) - 1);
       if (rank < LIST) list_lds[rank] = page;
@@ -266,7 +267,7 @@ __global__ __launch_bounds__(GIVE_THREADS) void fork_pages_kernel(PoolArgs a) {
       p = pair(i);
       wants = p.src >= 0 && p.begun && valid_page(a.table[(int64_t)p.src * a.table_width + p.whole], a.n_pages) >= 0;
     }
-    const int rank = wanted + sum_before(wants, all);
+    const int rank = wanted + sum_before<int>(wants, all);
     if (i < a.n) a.counts[i] = wants ? rank : p.src < 0 ? -2 : -1;
     wanted += all;
   }
@@ -325,9 +326,8 @@ __global__ __launch_bounds__(GIVE_THREADS) void reserve_pages_kernel(PoolArgs a)
   int64_t wanted = 0;
   for (int s0 = 0; s0 < a.n_seqs; s0 += GIVE_THREADS) {
     const int s = s0 + threadIdx.x;
-    int all;
-    const int mine = s < a.n_seqs ? a.counts[s] : 0;
-    const int64_t rank = wanted + sum_before(mine, all);
+    int64_t all;  // (of a thousand tables of two million entries each: beyond int32)
+    const int64_t rank = wanted + sum_before<int64_t>(s < a.n_seqs ? a.counts[s] : 0, all);
     if (s < a.n_seqs) a.counts[s] = (int)(rank < a.n_pages ? rank : a.n_pages);
     wanted += all;
   }
@@ -335,7 +335,7 @@ __global__ __launch_bounds__(GIVE_THREADS) void reserve_pages_kernel(PoolArgs a)
   for (int i = threadIdx.x; i < (had < LIST ? had : LIST); i += GIVE_THREADS) a.list[i] = list[i];
   if (threadIdx.x == 0) {
     a.counts[a.n_seqs] = had;
-    if (a.missing) *a.missing = (int)(wanted - had);
+    if (a.missing) *a.missing = (int)(wanted - had < INT_MAX ? wanted - had : INT_MAX);
   }
 }
 
@@ -343,13 +343,13 @@ __global__ __launch_bounds__(THREADS) void fill_kernel(PoolArgs a) {
   const int s = blockIdx.x * (THREADS / 64) + threadIdx.x / 64, lane = threadIdx.x & 63;
   if (s >= a.n_seqs) return;
   const int columns = columns_wanted(a, s), had = a.counts[a.n_seqs];
-  int rank = a.counts[s];
+  int64_t rank = a.counts[s];
   for (int c0 = 0; c0 < columns; c0 += 64) {
     const int c = c0 + lane;
     int32_t* entry = a.table + (int64_t)s * a.table_width + c;
     const bool lacks = c < columns && valid_page(*entry, a.n_pages) < 0;
     const unsigned long long all = __ballot(lacks);
-    const int at = rank + __popcll(all & ((1ull << lane) - 1));
+    const int64_t at = rank + __popcll(all & ((1ull << lane) - 1));
     if (lacks) *entry = at < had ? a.list[at] : -1;
     rank += __popcll(all);
   }
