@@ -674,7 +674,7 @@ int32_t moe_attention_tree(const moe_kv_cache* c, int32_t n_q_heads, int32_t T, 
 /* The accepted ones of a sequence's new tokens move up behind its base: place base[s] + keep[s, i] becomes place
  * base[s] + i, for i from 0 to the first negative keep[s, i] (device int32 [n_seqs, width], width 1..MOE_MAX_DRAFTS).
  * All of a sequence's rows are read before any is written, so keep may name them in any order and twice.  A place that
- * is not there is not read, and its row is left as it was, or not written.  new_lens (nullable, not base itself): base[s] + how many
+ * is not there is not read, and its row is left as it was, or not written.  new_lens (nullable, must not overlap base): base[s] + how many
  * were kept.  Sequences must not share the pages that are written. */
 int32_t moe_kv_compact(const moe_kv_cache* c, const int32_t* base, int32_t width, const int32_t* keep,
                        int32_t* new_lens, void* stream);

@@ -470,7 +470,9 @@ extern "C" int32_t moe_kv_compact(const moe_kv_cache* c, const int32_t* base, in
   if (width < 1 || width > MOE_MAX_DRAFTS) return fail(MOE_ERR_INVALID_ARG, "moe_kv_compact: width=%d outside 1..%d", width, MOE_MAX_DRAFTS);
   if (c->n_seqs == 0) return MOE_OK;
   if (!base || !keep) return fail(MOE_ERR_INVALID_ARG, "moe_kv_compact: base and keep must be non-NULL");
-  if (new_lens == base) return fail(MOE_ERR_INVALID_ARG, "moe_kv_compact: new_lens must not be base");
+  // (a workgroup writes a sequence's new length while others read the next ones' base)
+  if (new_lens && new_lens < base + c->n_seqs && base < new_lens + c->n_seqs)
+    return fail(MOE_ERR_INVALID_ARG, "moe_kv_compact: new_lens must not overlap base");
   CompactArgs a{};
   a.pool = pool_of(c, nullptr, nullptr);
   a.base = base;
