@@ -115,8 +115,14 @@ def _device(t, what: str) -> int:
 
 def _stream(stream, device: int) -> Optional[int]:
     """The given stream, or the device's current one; the raw handle spares a decoded token's calls the 2.7 us that building
-    torch's stream object takes, as much as all their other checks together."""
-    return (torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream) or None
+    torch's stream object takes, as much as all their other checks together.  A default stream has no handle of its own: the
+    library would launch on the current device, whatever device the tensors are on."""
+    handle = torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+    if stream is not None and stream.device_index != device:
+        raise ValueError(f"a stream of CUDA device {stream.device_index} for tensors on device {device}")
+    if not handle and torch._C._cuda_getDevice() != device:
+        raise ValueError(f"tensors on CUDA device {device}, whose default stream can only be used while it is the current device")
+    return handle or None
 
 
 class Rotary:
