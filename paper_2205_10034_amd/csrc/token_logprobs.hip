@@ -294,7 +294,8 @@ __device__ __forceinline__ void offer_groups(TopList& top, const uint32_t* found
   }
 }
 
-// The K largest of a row by one wavefront, chunk after chunk, where candidates are many (equal or rising logits): the bound rises on the way.
+// The K largest of a row by one wavefront, chunk after chunk, where candidates are many (equal or rising logits, fewer finite ones than K): the
+// bound rises on the way.  (20 of 576 rows of 128000 bfloat16 logits of which 5 are finite 72 us, of usual ones 40; one row of 50001 27 for 12.)
 template <typename X>
 __device__ __forceinline__ void find_in_order(TopList& top, uint32_t* found, const Candidates<X>& p) {
   const int lane = threadIdx.x & 63;
@@ -646,7 +647,8 @@ Division division_of(int T, int V, int K) {
   return d;
 }
 
-// What division_of wants for T rows and for any fewer: T parts, or as many more as rows are split into.
+// What division_of wants for T rows and for any fewer: T parts, or as many more as rows are split into.  (The type is not told: groups' maxima
+// have float32's four bytes.)
 size_t workspace_of(int T, int V, int K) {
   const int chunks = most_chunks(V, 16, 2);
   const int64_t split = (int64_t)T * most_parts(chunks), parts = !splits(chunks, K) ? 0 : split < MOST_PARTS ? split : MOST_PARTS;
@@ -747,9 +749,9 @@ __device__ __forceinline__ float pick(const X* kind, const u32x4 (&v)[loads<X>],
 //    few rows every group the sum for itself.
 //  - Of a token that is nearly certain r = sum_{j != id} p_j, by the group that has it: 1 - p without a difference, and log p = log(1 - r).
 // REGISTERS: a row has TEAM chunks or fewer, nothing is read twice.
-// Bound: HBM (8192 rows of 50001 bfloat16 logits 262 us, 6.2 TB/s read + written); of rows that are read again also the vector unit, for exp.  us of
-// usual rows / rows whose token has all but 1e-4 / rows far from zero:  8192 of 50001 bfloat16 262 / 350 / 434, 1000 of 32003 float32 40 / 55 / 80,
-// 1 of 262144 float32 9 / 18 / 21, 16384 of 1000 bfloat16 13 / 20 / 20.  In place: 329, 41, 26, 13 of usual ones, since a row is one group's.
+// Bound: HBM (8192 rows of 50001 bfloat16 logits 265 us, 6.2 TB/s read + written); of rows that are read again also the vector unit, for exp.  us of
+// usual rows / rows whose token has all but 1e-4 / rows far from zero:  8192 of 50001 bfloat16 265 / 352 / 434, 1000 of 32003 float32 39 / 54 / 79,
+// 1 of 262144 float32 8 / 16 / 19, 16384 of 1000 bfloat16 13 / 19 / 19.  In place: 328, 40, 23, 14 of usual ones, since a row is one group's.
 template <typename X, int TEAM, bool REGISTERS>
 __global__ __launch_bounds__(TEAM > WAVES ? 64 * TEAM : THREADS) void gradient_kernel(GradArgs a) {
   constexpr int BLOCK = TEAM > WAVES ? TEAM : WAVES;
@@ -776,8 +778,6 @@ __global__ __launch_bounds__(TEAM > WAVES ? 64 * TEAM : THREADS) void gradient_k
   int id = a.ids ? a.ids[t] : -1;
   const float lse = a.lse[t], ge = a.d_entropy ? a.d_entropy[t] : 0.f, gl = a.d_lse ? a.d_lse[t] : 0.f;
   float h = a.d_entropy ? a.entropy[t] : 0.f, g = a.d_logp ? a.d_logp[t] : 0.f;
-  u32x4 v[loads<X>];
-  load(c0 + me, v);
   if ((unsigned)id >= (unsigned)a.V || !a.d_logp) id = -1;
   if (id < 0) g = 0.f;
   if (ge == 0.f) h = 0.f;
@@ -791,6 +791,8 @@ __global__ __launch_bounds__(TEAM > WAVES ? 64 * TEAM : THREADS) void gradient_k
       for (int l = 0; l < loads<X>; ++l) store_some(y, index_of<X>(c, l, lane, back), a.V, u32x4{0, 0, 0, 0});
     return;
   }
+  u32x4 v[loads<X>];
+  load(c0 + me, v);  // (rows without a gradient are not read)
   if (g == 0.f) {
     id = -1;
     has_id = false;
