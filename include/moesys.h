@@ -663,8 +663,8 @@ typedef struct {
  * q, out [T, n_q_heads, head_dim], pointers and strides multiples of 16 bytes; out must not overlap q; lse (nullable)
  * device float [T, n_q_heads].  Rows of tokens that belong to no sequence are left as they were.  MOE_ERR_UNSUPPORTED
  * where T*n_q_heads or the work of one launch is beyond 2^26 - 4.  ws: moe_attention_tree_workspace_bytes, 256-byte
- * aligned, need not be cleared, one call at a time; that of a larger max_new serves a smaller one.  Results do not depend on what
- * else runs. */
+ * aligned, need not be cleared, one call at a time; that of a larger max_new serves a smaller one.  max_new decides how rows are dealt to
+ * workgroups, so it should be the step's own: 64 for steps of 4 takes two to three times as long.  Results do not depend on what else runs. */
 size_t moe_attention_tree_workspace_bytes(const moe_kv_cache* c, int32_t n_q_heads, int32_t max_new);
 int32_t moe_attention_tree(const moe_kv_cache* c, int32_t n_q_heads, int32_t T, int32_t max_new, const moe_head_rows* q,
                            const int32_t* token_first, const int32_t* seq_lens, const uint64_t* visible,
@@ -715,8 +715,9 @@ int32_t moe_kv_reserve(const moe_kv_cache* c, int32_t* refs, const int32_t* lens
  * rising index, and their log-probabilities.  A NaN ranks below all else.
  * A logit of -infinity is a token that cannot be: it adds nothing.  A row of nothing else has lse = logp = top_logp = -infinity
  * and entropy 0; a NaN or +infinity makes lse, logp, entropy and top_logp of its row NaN.
- * Sums are float32.  ws: moe_token_logprobs_workspace_bytes, 256-byte aligned, need not be cleared, one call at a time; that of
- * more rows, longer ones or more alternatives serves any call of fewer. */
+ * Sums are float32: what is next to 0 (logp and entropy of a token that is nearly certain) is off by some 2^-24.
+ * ws: moe_token_logprobs_workspace_bytes, 256-byte aligned, need not be cleared, one call at a time; that of more rows, longer
+ * ones or more alternatives serves any call of fewer. */
 size_t moe_token_logprobs_workspace_bytes(int32_t T, int32_t V, int32_t K);
 int32_t moe_token_logprobs(int32_t dtype, int32_t T, int32_t V, const void* x, int64_t row_stride, float scale,
                            const int32_t* ids, float* logp, float* lse, float* entropy, int32_t K, int32_t* top_ids,

@@ -60,7 +60,7 @@ def moe_attention_tree_workspace_bytes(cache: A.KVCache, n_q_heads: int, max_new
 def moe_attention_tree(cache: A.KVCache, q, token_first, seq_lens, out, ws, max_new: int, visible=None, scale: Optional[float] = None,
                        softcap: float = 0.0, window: int = 0, sinks: int = 0, slopes=None, lse=None, stream=None):
     """Attention of each sequence's new tokens: q, out [T, heads, head_dim], token_first int32 [sequences + 1], seq_lens int32
-    [sequences] (the new tokens counted), visible int64 [T] (bit j: the sequence's j-th new token; None: a chain), slopes
+    [sequences] (the new tokens counted), max_new the most new tokens of a sequence in this step, visible int64 [T] (bit j: the sequence's j-th new token; None: a chain), slopes
     float32 [heads] (optional), lse float32 [T, heads] (optional output)."""
     S, dtype, device = cache.n_seqs, cache.dtype, cache.device
     T, H = q.shape[0], q.shape[1]
